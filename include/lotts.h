@@ -285,6 +285,135 @@ int skinny_gemm_append(int32_t B, int32_t k, int32_t Hkv, int32_t D, int32_t N, 
                        void *stream);
 
 /*
+ * Geometry of one verify_attention_paged call: a cache in pages of page_tokens tokens, found through a page table.
+ * Key t of branch b is row t % page_tokens of page page_table[b][t / page_tokens], in Kpages and Vpages alike.
+ * Strides are in ELEMENTS (the table's: in entries), multiples of 16 bytes; the innermost D elements of every row are contiguous; 0
+ * selects the dense layout.  K and V use the same strides.
+ */
+typedef struct {
+    int32_t B;            /* branches, 1 .. 4096 */
+    int32_t T;            /* rows of Q and O: new tokens of all branches together, >= 1; T * Hq < 2^24 */
+    int32_t max_new;      /* no branch has more new tokens than this; 1 <= max_new <= T */
+    int32_t Hq, Hkv;      /* query / KV heads, Hq % Hkv == 0; query head h reads KV head h / (Hq / Hkv) */
+    int32_t D;            /* head dimension: 64 or 128 */
+    int32_t page_tokens;  /* tokens of a page: a power of two from 16 to 1024 */
+    int32_t pages;        /* pages of the pool, 1 .. 2^24 */
+    int32_t columns;      /* entries of a branch's row of the table; columns * page_tokens < 2^30 */
+    int32_t dtype;        /* lotts_dtype of Q, K, V and O */
+    float scale;          /* softmax scale; 0 selects 1 / sqrt(D) */
+    int64_t q_stride_t, q_stride_h;                           /* Q [T][Hq][D] */
+    int64_t page_stride_p, page_stride_h, page_stride_t;      /* Kpages, Vpages [pages][Hkv][page_tokens][D] */
+    int64_t table_stride;                                     /* page_table [B][columns] */
+    int64_t o_stride_t, o_stride_h;                           /* O [T][Hq][D] */
+} lotts_paged_desc;
+
+/* Bytes of workspace verify_attention_paged needs for this geometry; 0 if the descriptor is invalid. */
+size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc *desc);
+
+/*
+ * verify_attention_paged -- causal attention of the new tokens of every branch over its paged cache, one layer.  The branches of a call may
+ * have different numbers of new tokens: chunks of prompts that are being read, drafts that are verified (Section 2), single tokens of plain
+ * decoding.  Branches of one question share the pages of what they have in common (Section 3.2).
+ *
+ *   O[q_start[b] + i][h][:] = sum_t softmax_t(scale * <Q[q_start[b] + i][h], K_t>) * V_t
+ * for i = 0 .. n - 1, n = q_start[b + 1] - q_start[b], over the keys t = 0 .. kv_len[b] - n + i of branch b (the last n tokens of the branch are
+ * the new ones; token i sees itself and the earlier ones).  Keys whose table entry lies outside [0, pages) are not seen.  A row that
+ * sees nothing at all is 0, its lse -infinity.
+ *
+ *   Q, O          [T][Hq][D]  dtype, strides from desc; rows of O that belong to no branch are left as they were
+ *   Kpages, Vpages [pages][Hkv][page_tokens][D] dtype
+ *   page_table    [B][columns] int32 (device); entries behind a branch's last token are not looked at
+ *   kv_len        [B] int32 (device): tokens of branch b INCLUDING its new ones, 0 .. columns * page_tokens
+ *   q_start       [B + 1] int32 (device): first row of each branch's new tokens, ascending from 0, q_start[B] <= T; equal neighbours:
+ *                 a branch without new tokens.  NULL: every branch has T / B of them (T % B == 0, max_new = T / B)
+ *   lse           [T][Hq] fp32, out, may be NULL: natural-log sum of exp of the scaled scores
+ *   workspace     >= verify_attention_paged_workspace_bytes(desc), 16-byte aligned; as for verify_attention: zero-filled once before its
+ *                 first use, then this entry point's own, shared by calls that are ordered on one stream
+ * kv_len, q_start and the table are device data and are not checked on the host: the kernels keep whatever they address inside the buffers
+ * that the descriptor describes, but the rows of a branch whose data break the contract are then unspecified.
+ * What a cache row holds behind the branch's last token does not matter, NaN included.  (A row's weight for a later token of the same
+ * chunk is exactly 0; in bf16 an infinity or NaN among the chunk's own V rows reaches the rows in front of it all the same.)
+ * bf16 inputs are multiplied on the matrix cores with fp32 accumulation; fp32 inputs are computed in fp32 throughout.
+ */
+int verify_attention_paged(const lotts_paged_desc *desc, const void *Q, const void *Kpages, const void *Vpages, const int32_t *page_table,
+                           const int32_t *kv_len, const int32_t *q_start, void *O, float *lse, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
+/*
+ * kv_append_paged -- the K and V rows of the new tokens of every branch go to their places in the paged cache, where
+ * verify_attention_paged expects them: row q_start[b] + i of Knew and Vnew to key kv_len[b] - n + i of branch b, n = q_start[b + 1] - q_start[b].
+ *   Knew, Vnew: [T][Hkv][D] views (element strides new_stride_t / _h, D contiguous); V uses the same strides as K
+ *   Kpages, Vpages: [pages][Hkv][page_tokens][D] in/out (element strides page_stride_p / _h / _t, none of them 0 by default)
+ *   page_table [B][columns], kv_len [B], q_start [B + 1] or NULL: as for verify_attention_paged
+ *   dtype: LOTTS_BF16 or LOTTS_F32; a row of D elements is a multiple of 16 bytes; pointers and strides are 16-byte aligned
+ * Tokens whose place lies in front of 0, behind the table's columns or in no page are skipped.  A plain copy: bit-exact; nothing else in the
+ * pages is touched.  No two branches may write to one page: kv_pages_reserve sees to that.
+ */
+int kv_append_paged(int32_t B, int32_t T, int32_t Hkv, int32_t D, int32_t page_tokens, int32_t pages, int32_t columns, lotts_dtype dtype,
+                    const void *Knew, const void *Vnew, int64_t new_stride_t, int64_t new_stride_h, void *Kpages, void *Vpages,
+                    int64_t page_stride_p, int64_t page_stride_h, int64_t page_stride_t, const int32_t *page_table, int64_t table_stride,
+                    const int32_t *kv_len, const int32_t *q_start, void *stream);
+
+/*
+ * Upkeep of a paged cache.  Its state is device data of the caller's:
+ *   page_table [B][columns] int32 (row stride table_stride >= columns): page numbers; an entry outside [0, pages) is no page (-1 is what
+ *              these calls write).  B <= 4096, pages <= 2^24
+ *   refs       [pages] int32: how many table entries name the page; 0: the page is free.  The calls keep it so; a caller who holds
+ *              pages by other means adds its own references
+ *   kv_len     [B] int32: tokens of each branch
+ * One table serves all layers: page p of every layer's K and V belongs to it.  All results are whole numbers that do not depend on timing.
+ * Calls on the same state are ordered on one stream.  workspace: >= kv_pages_workspace_bytes(pages), 4-byte aligned, any contents.
+ */
+size_t kv_pages_workspace_bytes(int32_t pages);
+
+/*
+ * kv_pages_reserve -- room for new_tokens[b] (>= 0) more tokens of every branch, whose lengths grow by as many.  Every page that they will be
+ * written to is the branch's alone afterwards: where the table has none, and where the page is shared, it gets a free one (the
+ * free pages with the lowest numbers, in the order of branches and columns).  A shared page that holds tokens to keep has to be copied:
+ * copies[b] = (from, to), at most one a branch, (-1, -1) for none; kv_pages_copy takes them as they are, before the next call that
+ * changes the state.
+ *   copies [B][2] int32 out;  missing [1] int32 out: 0, or nothing has been changed: > 0, so many free pages were lacking; -1, a
+ *   branch's tokens would pass the table's columns
+ */
+int kv_pages_reserve(int32_t B, int32_t columns, int32_t pages, int32_t page_tokens, int32_t *page_table, int64_t table_stride, int32_t *refs,
+                     int32_t *kv_len, const int32_t *new_tokens, int32_t *copies, int32_t *missing, void *workspace, size_t workspace_bytes,
+                     void *stream);
+
+/*
+ * kv_pages_fork -- branch b becomes what branch parent[b] was before the call: it names the same pages and has the same length (Section 3.2:
+ * the branches of a question start from one prompt).  parent[b] = b or >= B leaves the branch as it is, < 0 empties it; branches may
+ * change places.  No page is copied; references follow.
+ */
+int kv_pages_fork(int32_t B, int32_t columns, int32_t pages, int32_t *page_table, int64_t table_stride, int32_t *refs, int32_t *kv_len,
+                  const int32_t *parent, void *stream);
+
+/*
+ * kv_pages_free -- branch b is cut to min(kv_len[b], keep[b]) tokens (keep NULL: to kv_len[b], as an acceptance has rolled it back), and gives
+ * up the pages behind them; keep[b] <= 0 ends the branch.
+ */
+int kv_pages_free(int32_t B, int32_t columns, int32_t pages, int32_t page_tokens, int32_t *page_table, int64_t table_stride, int32_t *refs,
+                  int32_t *kv_len, const int32_t *keep, void *stream);
+
+/*
+ * kv_pages_compact -- the pages in use become pages 0 .. n - 1, n their number: those from n on, in ascending order, take the places of the
+ * free ones below n, in ascending order; table and references follow.  The data move by kv_pages_copy with the same pairs.
+ *   moves [max(1, pages / 2)][2] int32 out: (from, to); rows behind the last pair are left as they were
+ *   counts [2] int32 out: number of pairs, n
+ */
+int kv_pages_compact(int32_t B, int32_t columns, int32_t pages, int32_t *page_table, int64_t table_stride, int32_t *refs, int32_t *moves,
+                     int32_t *counts, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * kv_pages_copy -- copies whole pages, in every plane (a layer's K or V) of a pool: page pairs[j][1] gets what page pairs[j][0] holds,
+ * j = 0 .. n - 1, or min(n, count[0]) - 1 if count (device) is not NULL.  Pairs with a number outside [0, pages) are skipped.  No page is
+ * written to that another pair of the call reads or writes.
+ *   pool: planes * pages pages of page_bytes bytes (plane_stride, page_stride in BYTES); all multiples of 16, 16-byte aligned
+ *   pairs [n][2] int32 (device)
+ */
+int kv_pages_copy(void *pool, int32_t planes, int32_t pages, int64_t plane_stride, int64_t page_stride, int64_t page_bytes, const int32_t *pairs,
+                  int32_t n, const int32_t *count, void *stream);
+
+/*
  * Kernel timer -- device execution time of the kernels the entry points launch, for callers that
  * have no profiler at hand (not an operation of the paper; a measurement aid).
  * Between lotts_timer_start and lotts_timer_stop every kernel launched by the CALLING HOST THREAD
@@ -302,7 +431,8 @@ int skinny_gemm_append(int32_t B, int32_t k, int32_t Hkv, int32_t D, int32_t N, 
  * partials from prefix items (4 P > Lmax) or from several row groups, but for the smallest batches);
  * spec_accept 1 (2 -- scan, pick -- when V is beyond 2^18); spec_accept_logits 2 (row statistics, scan and
  * pick); majority_vote 1; confidence_vote 1; skinny_gemm 1 (2 when K is split: GEMM, reduce),
- * skinny_gemm_append the same (and kv_append where a product that streams W has K unsplit).
+ * skinny_gemm_append the same (and kv_append where a product that streams W has K unsplit); verify_attention_paged 1; kv_append_paged 1;
+ * kv_pages_reserve, _fork, _free, _copy 1; kv_pages_compact 2.
  */
 int lotts_timer_start(int32_t max_launches);
 int lotts_timer_pause(int32_t paused);
