@@ -6,6 +6,7 @@
 // A branch's query rows of one KV head -- n new tokens x G query heads, the heads of a token next to each other -- are stacked, and a
 // workgroup takes a tile of that stack.  Row r of the stack is token r / G; it sees the keys in front of position L - n + r / G + 1.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "lotts_common.h"
@@ -17,35 +18,49 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPgMaxBranches = 4096;
 constexpr int kPgMaxPages = 1 << 24;
 constexpr int kPgThreads = 256;
 constexpr int kPgWaves = kPgThreads / kWave;
-constexpr int kPgGroup = 16;  // keys that lie in one page whatever the page size: what one wavefront loads of a tile
+constexpr int kPgGroup = 16;         // keys that lie in one page whatever the page size
+constexpr int kNarrowTile = 32;      // keys of a tile of a narrow item: one wavefront's at a time
+constexpr int kWideTile = 64;        // keys of a tile of a wide item: the workgroup's
+constexpr int kWideRows = 256;       // rows of a wide item
+// Places in the sequence of work (below) of a narrow tile, a wide tile, and what starting on an item costs.
+constexpr int kNarrowCost = 2, kWideCost = 5, kStartCost = 6;
+constexpr int kMinPiece = 32;        // least places of a worker
+constexpr int kMergeGroup = 8;       // partials that are merged at a time
 
 struct PagedParams {
     const void *Q, *K, *V;
     const int32_t *table, *kv_len, *q_start;
-    void* O;
-    float* lse;
-    long long q_t, q_h, o_t, o_h;       // bytes
+    long long q_t, q_h;                 // bytes
     long long page_p, page_h, page_t;   // bytes
     long long table_stride;
     int B, T, R, Hq, Hkv, G, pages, columns, shift;
-    int tiles;                          // row tiles of a KV head, at most
+    int items;                          // item slots of a KV head
+    int workers;
     float scale_log2;                   // scale * log2(e)
-    FastDiv d_hkv, d_g;
+    FastDiv d_g;
+    void* O;
+    float* lse;
+    long long o_t, o_h;                 // bytes
+    void* ws;                           // partials: 2 * workers slots of part_rows rows of D floats, then as many of (maximum, sum)
+    unsigned ws_bytes, off_ml, off_o;
+    int part_rows;
+    unsigned long long* cells;          // arrivals: [2][2 * workers], (call tag << 16) | arrivals
+    unsigned long long tag;
 };
 
 // A branch of the call: its first row of Q, its new tokens and all its tokens (both brought into the range that the arguments allow, so
 // that nothing is addressed out of bounds whatever the device data say).
 struct Branch {
-    int b, first, n, L;
+    int first, n, L;
 };
 __device__ __forceinline__ Branch branch_at(const PagedParams& p, int b) {
     Branch r;
-    r.b = b;
     int end;
     if (p.q_start) {
         r.first = min(max(p.q_start[b], 0), p.T);
@@ -58,193 +73,609 @@ __device__ __forceinline__ Branch branch_at(const PagedParams& p, int b) {
     r.L = min(max(p.kv_len[b], 0), p.columns << p.shift);
     return r;
 }
-// Row tiles: branch b's are numbers floor(q_start[b] * G / rows) + b and on; enough for its ceil(n * G / rows), and no sum over the branches
-// is needed to find whose a number is.
-__device__ __forceinline__ int first_tile(const PagedParams& p, int b, int rows) {
-    const int first = p.q_start ? min(max(p.q_start[b], 0), p.T) : b * p.R;
-    return (int)((long long)first * p.G / rows) + b;
-}
-__device__ __forceinline__ int branch_of_tile(const PagedParams& p, int tile, int rows, int lane) {
-    int first = 0;
-    if (p.B > kWave) {
-        const int b = lane * kWave;
-        first = kWave * max(0, __popcll(__ballot(b < p.B && first_tile(p, min(b, p.B - 1), rows) <= tile)) - 1);
-    }
-    const int b = first + lane;
-    return max(0, first + __popcll(__ballot(b < p.B && first_tile(p, min(b, p.B - 1), rows) <= tile)) - 1);
-}
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* base, unsigned bytes) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+}
+// Partials cross workgroups inside the launch: device scope (sc0 sc1).
+constexpr int kDevScope = 17;
+__device__ __forceinline__ void part_store4(__amdgpu_buffer_rsrc_t r, unsigned at, float4 v) {
+    u32x4 u;
+    u[0] = __float_as_uint(v.x); u[1] = __float_as_uint(v.y); u[2] = __float_as_uint(v.z); u[3] = __float_as_uint(v.w);
+    __builtin_amdgcn_raw_buffer_store_b128(u, r, (int)at, 0, kDevScope);
+}
+__device__ __forceinline__ void part_store2(__amdgpu_buffer_rsrc_t r, unsigned at, float2 v) {
+    u32x2 u;
+    u[0] = __float_as_uint(v.x); u[1] = __float_as_uint(v.y);
+    __builtin_amdgcn_raw_buffer_store_b64(u, r, (int)at, 0, kDevScope);
+}
+__device__ __forceinline__ float4 part_load4(__amdgpu_buffer_rsrc_t r, unsigned at) {
+    const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, kDevScope);
+    return make_float4(__uint_as_float(u[0]), __uint_as_float(u[1]), __uint_as_float(u[2]), __uint_as_float(u[3]));
+}
+__device__ __forceinline__ float2 part_load2(__amdgpu_buffer_rsrc_t r, unsigned at) {
+    const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, 0, kDevScope);
+    return make_float2(__uint_as_float(u[0]), __uint_as_float(u[1]));
+}
+
+// ---------------------------------------------------------------------------------------------
+// The work of a call.  A KV head's items -- the row tiles of its branches, one after the other -- form a sequence in which every key tile
+// takes as many places as it takes time, all heads' sequences follow one another, and worker w of W gets the w-th of equal pieces of
+// the whole, whatever the branches' lengths and numbers of new tokens are.  Where a piece ends inside an item, the item has a partial
+// result from either side.  Nothing of this is known to the host: every workgroup finds its piece from the lengths of all branches,
+// 64 item slots at a time, a lane each.
+//   Items are narrow (all rows of a branch, at most NARROW_TILES * 32: the keys are dealt to the wavefronts) or wide (kWideRows rows: the rows
+//   are dealt to them).  The slots of branch b begin at floor(q_start[b] * G / kWideRows) + b, which leaves room for its ceil(n * G / kWideRows)
+//   items and needs no sum over the branches; a narrow branch uses the first of its slots.  Without wide items a slot is a branch.
+// ---------------------------------------------------------------------------------------------
+struct Items {        // of the lane
+    unsigned end;     // places of the head's sequence up to the end of this item
+    int b, first, n, L, row0, tiles, cost;
+};
+template <bool WIDE>
+__device__ __forceinline__ int first_slot(const PagedParams& p, int b) {
+    if (!WIDE) return b;
+    const int first = p.q_start ? min(max(p.q_start[b], 0), p.T) : b * p.R;
+    return (int)((long long)first * p.G / kWideRows) + b;
+}
+template <bool WIDE, int NARROW_TILES>
+__device__ __forceinline__ Items items_at(const PagedParams& p, int base, unsigned before, int lane) {
+    const int slot = base + lane;
+    Items t;
+    int b = min(slot, p.B - 1);
+    if (WIDE) {  // the last branch whose slots begin at or before this one
+        int lo = 0, hi = p.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (first_slot<true>(p, mid) <= slot) lo = mid;
+            else hi = mid - 1;
+        }
+        b = lo;
+    }
+    const Branch br = branch_at(p, b);
+    const int rows = br.n * p.G;
+    const bool narrow = !WIDE || rows <= NARROW_TILES * 32;
+    const int j = slot - first_slot<WIDE>(p, b);
+    t.row0 = j * kWideRows;
+    const bool there = slot < p.items && (narrow ? j == 0 && rows > 0 : j >= 0 && t.row0 < rows);
+    const int end = narrow ? rows : min(t.row0 + kWideRows, rows);
+    const int keys = max(1, br.L - br.n + quot(max(end, 1) - 1, p.d_g) + 1);
+    t.b = b; t.first = br.first; t.n = br.n; t.L = br.L;
+    t.tiles = narrow ? (keys - 1) / kNarrowTile + 1 : (keys - 1) / kWideTile + 1;
+    t.cost = there ? kStartCost + t.tiles * (narrow ? kNarrowCost : kWideCost) : 0;
+    t.end = before + wave_incl_scan_u32((unsigned)t.cost);
+    return t;
+}
+
+// Pieces: any rising function of w does as long as all agree on it.
+struct Pieces {
+    double places;
+    int workers;
+    __device__ __forceinline__ long long start(int w) const { return (long long)(places * w / workers); }
+    __device__ __forceinline__ int worker(long long at) const {
+        int w = min((int)((double)at * workers / places), workers - 1);
+        while (w > 0 && start(w) > at) --w;
+        while (w + 1 < workers && start(w + 1) <= at) ++w;
+        return w;
+    }
+};
+
+// A part of an item: rows [row0, row0 + nrows) of the stack of (branch, KV head) against the key tiles [lo, hi) of its `tiles`.
+struct Segment {
+    int b, kvh, first, n, L, row0, nrows;
+    int lo, hi, tiles;
+    int w0, parts;  // the workers that have tiles of the item: w0 .. w0 + parts - 1
+};
+
+// Output quad c4 of row r of a segment: normalised and rounded; the first quad's thread stores the lse.
+__device__ __forceinline__ void store_out(const PagedParams& p, const Segment& g, int r, int c4, float4 o, float M, float l) {
+    const int i = quot(g.row0 + r, p.d_g), h = g.kvh * p.G + g.row0 + r - i * p.G;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing is 0
+    bf16x4 v;
+    v[0] = (__bf16)(o.x * inv);
+    v[1] = (__bf16)(o.y * inv);
+    v[2] = (__bf16)(o.z * inv);
+    v[3] = (__bf16)(o.w * inv);
+    *reinterpret_cast<bf16x4*>((unsigned char*)p.O + (long long)(g.first + i) * p.o_t + h * p.o_h + c4 * 8) = v;
+    if (p.lse && c4 == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (M + log2f(l)) * 0.69314718055994530942f;
+}
+
+// Slot of worker w's partial of an item: a worker has at most one item that it begins and does not end, and one that it goes on with.
+__device__ __forceinline__ int part_slot(int w, int w0) { return 2 * w + (w == w0 ? 1 : 0); }
+
+// Merges partials [from, from + count) of the segment's item -- every STEP-th of them -- in their order: into the output, or in place of the first.
+template <int D>
+__device__ __forceinline__ void merge_parts(const PagedParams& p, const Segment& g, __amdgpu_buffer_rsrc_t rs, int from, int count, int step, bool last) {
+    constexpr int F4 = D / 4, CH = 8;
+    for (int e = threadIdx.x; e < g.nrows * F4; e += kPgThreads) {  // (a row's quads lie in one wavefront: what is read comes in front of what is written)
+        const int r = e / F4, c4 = e - r * F4;
+        float M = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        unsigned first_at = 0;
+        for (int s0 = 0; s0 < count; s0 += CH) {
+            float2 ml[CH];
+            float4 v[CH];
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                ml[j] = make_float2(-INFINITY, 0.f);
+                v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (s0 + j < count) {
+                    const unsigned row = (unsigned)part_slot(g.w0 + from + (s0 + j) * step, g.w0) * p.part_rows + r;
+                    if (s0 + j == 0) first_at = row;
+                    ml[j] = part_load2(rs, p.off_ml + row * 8u);
+                    v[j] = part_load4(rs, p.off_o + (row * D + c4 * 4) * 4u);
+                }
+            }
+            float Mn = M;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) Mn = fmaxf(Mn, ml[j].x);
+            const float Mu = Mn == -INFINITY ? 0.f : Mn, a = __builtin_amdgcn_exp2f(M - Mu);
+            l *= a;
+            o.x *= a; o.y *= a; o.z *= a; o.w *= a;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const float w = __builtin_amdgcn_exp2f(ml[j].x - Mu);
+                l += ml[j].y * w;
+                o.x += v[j].x * w; o.y += v[j].y * w; o.z += v[j].z * w; o.w += v[j].w * w;
+            }
+            M = Mn;
+        }
+        if (last) {
+            store_out(p, g, r, c4, o, M, l);
+        } else {
+            part_store4(rs, p.off_o + (first_at * D + c4 * 4) * 4u, o);
+            if (c4 == 0) part_store2(rs, p.off_ml + first_at * 8u, make_float2(M, l));
+        }
+    }
+}
+
+// The workgroup's partial of a cut item is written: it counts itself, and whoever comes last merges -- kMergeGroup neighbours first, then what
+// these have left.  Every wavefront waits for its stores before the count.  A cell starts at the call's tag, which is larger than that
+// of any earlier call, and goes back to zero: a captured launch is replayed with its tag.
+template <int D>
+__device__ __forceinline__ void arrive(const PagedParams& p, const Segment& g, __amdgpu_buffer_rsrc_t rs, int w, int* sh) {
+    auto last_of = [&](unsigned long long* cell, int count) {
+        __builtin_amdgcn_s_waitcnt(0);  // the wavefront's stores are in memory
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            atomicMax(cell, p.tag);
+            const bool last = atomicAdd(cell, 1ull) + 1 == p.tag + count;
+            if (last) __hip_atomic_store(cell, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *sh = last;
+        }
+        __syncthreads();
+        const bool last = *sh != 0;
+        __syncthreads();
+        return last;
+    };
+    const int at = w - g.w0, group = at / kMergeGroup, first = group * kMergeGroup, members = min(kMergeGroup, g.parts - first);
+    const bool one_group = g.parts <= kMergeGroup;
+    if (members > 1) {
+        if (!last_of(p.cells + part_slot(g.w0 + first, g.w0), members)) return;
+        merge_parts<D>(p, g, rs, first, members, 1, one_group);
+    }
+    if (one_group) return;
+    const int groups = (g.parts - 1) / kMergeGroup + 1;
+    if (!last_of(p.cells + 2 * p.workers + part_slot(g.w0, g.w0), groups)) return;
+    merge_parts<D>(p, g, rs, 0, groups, kMergeGroup, true);
+}
+
+// What a wavefront knows of the pages of the tiles ahead: lane i has the entries of the i-th tile from `base` on, STEP tiles apart.  One load
+// for 64 tiles, so that no tile waits for its entry.
+__device__ __forceinline__ int page_entry(const PagedParams& p, const int32_t* row, int key) { return row[min(key >> p.shift, p.columns - 1)]; }
+
+// 16 keys of a page: the buffer ends behind the last one that there is, so that keys behind it, and those without a page, read as zeros.
+__device__ __forceinline__ unsigned group_bytes(const PagedParams& p, int entry, int key, int keys, int row_bytes) {
+    const int n = (unsigned)entry < (unsigned)p.pages ? min(keys - key, kPgGroup) : 0;
+    return n > 0 ? (unsigned)(n - 1) * (unsigned)p.page_t + row_bytes : 0;
+}
+__device__ __forceinline__ long long group_at(const PagedParams& p, int entry, int key, int kvh) {
+    return (long long)((unsigned)entry < (unsigned)p.pages ? entry : 0) * p.page_p + kvh * p.page_h + (key & ((1 << p.shift) - 1)) * p.page_t;
 }
 
 // ---------------------------------------------------------------------------------------------
 // bf16
 // ---------------------------------------------------------------------------------------------
+template <int D>
+struct Tile {
+    static constexpr int KS = D / 16;             // MFMA k-steps of the QK^T contraction
+    static constexpr int DB = D / 32;             // 32-wide blocks of the head dimension
+    static constexpr int LPR = D / 8;             // lanes per key row of a load
+    static constexpr int RPI = kWave / LPR;       // key rows per load instruction
+    static constexpr int NLD = kPgGroup / RPI;    // load instructions per 16 keys
+    static constexpr int KSTRIDE = D * 2 + 16;    // bytes per key row in LDS (pad: conflict-free 16-byte row reads)
+    static constexpr int VSTRIDE = D * 2 + 64;    // (pad: conflict-free transposing reads)
+    static constexpr int OSTRIDE = D + 4;         // floats per row of a parked output
+    static constexpr int SLAB = kNarrowTile * (KSTRIDE + VSTRIDE);  // LDS of a wavefront (narrow)
+    static constexpr int LDS = kPgWaves * SLAB;
+    static_assert(32 * OSTRIDE * 4 <= SLAB, "a parked output reuses the wavefront's slab");
+    static_assert(kWideTile * (KSTRIDE + VSTRIDE) <= LDS, "a wide tile fits");
+};
+
+// One row tile's step: scores of 32 keys, mask, running maximum and sum; the weights come back in the order in which the product with V takes
+// them.  Register i of a lane is key (i / 4) * 8 + hh * 4 + i % 4 of the tile, for row `lane % 32`; vis: keys in front of it are seen;
+// have: bit g: 16 keys from 16 g on lie in a page.
+template <int DB>
+__device__ __forceinline__ void softmax_step(f32x16& s, f32x16 (&o)[DB], float& m, float& l, bf16x8 (&pf)[2], float scale, int vis, int have, bool masked) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] *= scale;
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (i >> 2) * 8 + (i & 3) < vis && (have >> (i >> 3) & 1) ? s[i] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx = fmaxf(mx, shfl_xor_f(mx, 32));
+    const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float w = __builtin_amdgcn_exp2f(s[i] - m_use);
+        sum += w;
+        pf[i >> 3][i & 7] = (__bf16)w;  // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
+    }
+    l = l * alpha + sum;
+    m = m_new;
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {  // (seldom, once some hundred keys have gone by)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
+}
+
+template <int D>
+__device__ __forceinline__ bf16x8 read_v(const unsigned char* at) {
+    union {
+        short4v s[2];
+        bf16x8 v;
+    } f;
+    f.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(at));
+    f.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(at + 8 * Tile<D>::VSTRIDE));
+    return f.v;
+}
+
+// A narrow item's part: wavefront w takes tiles lo + w, lo + w + 4, ..., each into registers one tile ahead and through a slab of its own.
 template <int D, int TW>
-__global__ __launch_bounds__(kPgThreads, 1) void paged_attn_kernel(const PagedParams p) {
-    constexpr int KT = 64;                  // keys of a tile
-    constexpr int ROWS = kPgWaves * TW * 32;
-    constexpr int KS = D / 16, DB = D / 32;
-    constexpr int LPR = D / 8, RPI = kWave / LPR, NLD = kPgGroup / RPI;
-    constexpr int KSTRIDE = D * 2 + 16, VSTRIDE = D * 2 + 64;
-    __shared__ __attribute__((aligned(16))) unsigned char kslab[KT * KSTRIDE];
-    __shared__ __attribute__((aligned(16))) unsigned char vslab[KT * VSTRIDE];
+__device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh) {
+    using X = Tile<D>;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     const int ln = lane & 31, hh = lane >> 5;
-    const int id = (int)blockIdx.x, item = quot(id, p.d_hkv), kvh = id - item * p.Hkv;
-    const int tile_no = p.tiles - 1 - item;  // the rows that see most first
-    const int b = __builtin_amdgcn_readfirstlane(branch_of_tile(p, tile_no, ROWS, lane));
-    const Branch br = branch_at(p, b);
-    const int rows = br.n * p.G, row0 = (tile_no - first_tile(p, b, ROWS)) * ROWS;
-    if (row0 < 0 || row0 >= rows) return;
-    const int before = br.L - br.n;  // row r sees the keys in front of before + r / G + 1
-
-    // the wavefront's rows
-    bf16x8 qf[TW][KS];
+    const int32_t* row = p.table + g.b * p.table_stride;
+    const int keys = min(g.L, max(0, g.L - g.n + quot(g.nrows - 1, p.d_g) + 1)), before = g.L - g.n;
+    const int n_tiles = g.lo + wave < g.hi ? (g.hi - 1 - g.lo - wave) / kPgWaves + 1 : 0;
+    const int v_row = lane / X::LPR, v_chunk = lane % X::LPR;
+    const int blk = lane >> 4, i16 = lane & 15;
+    const int tr_off = ((blk >> 1) * 4 + (i16 >> 2)) * X::VSTRIDE + ((blk & 1) * 16 + (i16 & 3) * 4) * 2;
+    unsigned char *kslab = lds + wave * X::SLAB, *vslab = kslab + kNarrowTile * X::KSTRIDE;
+    int ahead[2], ahead_from = 0;  // entries of the wavefront's tiles ahead_from .. ahead_from + 63
+    auto look_ahead = [&](int it) {
+        ahead_from = it;
+        const int key = (g.lo + wave + (it + lane) * kPgWaves) * kNarrowTile;
+        ahead[0] = page_entry(p, row, key);
+        ahead[1] = page_entry(p, row, key + kPgGroup);
+    };
+    u32x4 kst[2][X::NLD], vst[2][X::NLD];
+    int have_next = 0;
+    auto fetch = [&](int it) {
+        if (it - ahead_from >= kWave) look_ahead(it);
+        const int kb = (g.lo + wave + it * kPgWaves) * kNarrowTile;
+        have_next = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int key = kb + h * kPgGroup, e = __builtin_amdgcn_readlane(ahead[h], it - ahead_from);
+            const unsigned bytes = group_bytes(p, e, key, keys, D * 2);
+            const long long at = group_at(p, e, key, g.kvh);
+            have_next |= (unsigned)e < (unsigned)p.pages ? 1 << h : 0;
+            const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes), vr = buffer((const unsigned char*)p.V + at, bytes);
+#pragma unroll
+            for (int i = 0; i < X::NLD; ++i) {
+                const unsigned off = (unsigned)(i * X::RPI + v_row) * (unsigned)p.page_t + v_chunk * 16;
+                kst[h][i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (int)off, 0, 2);
+                vst[h][i] = __builtin_amdgcn_raw_buffer_load_b128(vr, (int)off, 0, 2);
+            }
+        }
+    };
+    if (n_tiles > 0) look_ahead(0);
+    bf16x8 qf[TW][X::KS];
     int lim[TW];
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
-        const int r = min(row0 + (wave * TW + t) * 32 + ln, rows - 1);
-        const int i = quot(r, p.d_g), g = r - i * p.G;
+        const int r = min(t * 32 + ln, g.nrows - 1), i = quot(r, p.d_g);
         lim[t] = before + i + 1;
-        const unsigned char* qp = (const unsigned char*)p.Q + (br.first + i) * p.q_t + (kvh * p.G + g) * p.q_h;
+        const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
+        for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
     }
-    const int last = quot(min(row0 + ROWS, rows) - 1, p.d_g);
-    const int keys = max(0, before + last + 1), n_tiles = (keys + KT - 1) / KT;
-
-    const int v_row = lane / LPR, v_chunk = lane % LPR;
-    const int blk = lane >> 4, i16 = lane & 15;
-    const int tr_off = ((blk >> 1) * 4 + (i16 >> 2)) * VSTRIDE + ((blk & 1) * 16 + (i16 & 3) * 4) * 2;
-    const int32_t* row = p.table + b * p.table_stride;
-    auto entry = [&](int key) { return __builtin_amdgcn_readfirstlane(row[min(key >> p.shift, p.columns - 1)]); };
-    u32x4 kst[NLD], vst[NLD];
-    int have = 0, have_next = 0;  // which groups of a tile lie in a page
-    auto fetch = [&](int kb) {
-        have_next = 0;
-        int e = 0;
-#pragma unroll
-        for (int g = 0; g < KT / kPgGroup; ++g) {
-            const int eg = entry(kb + g * kPgGroup);
-            if ((unsigned)eg < (unsigned)p.pages) have_next |= 1 << g;
-            if (g == wave) e = eg;
-        }
-        const int key = kb + wave * kPgGroup;
-        const int n = (have_next >> wave & 1) ? min(keys - key, kPgGroup) : 0;
-        // keys behind the last one, and those without a page, are out of the buffer's range: they read as zeros
-        const unsigned bytes = n > 0 ? (unsigned)((n - 1) * p.page_t) + D * 2 : 0;
-        const long long at = (n > 0 ? e : 0) * p.page_p + kvh * p.page_h + (key & ((1 << p.shift) - 1)) * p.page_t;
-        const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes), vr = buffer((const unsigned char*)p.V + at, bytes);
-#pragma unroll
-        for (int i = 0; i < NLD; ++i) {
-            const unsigned off = (unsigned)((i * RPI + v_row) * p.page_t) + v_chunk * 16;
-            kst[i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (int)off, 0, 0);
-            vst[i] = __builtin_amdgcn_raw_buffer_load_b128(vr, (int)off, 0, 0);
-        }
-    };
-
-    f32x16 oacc[TW][DB];
+    if (n_tiles > 0) fetch(0);
+    const bool two = TW > 1 && g.nrows > 32;
+    f32x16 oacc[TW][X::DB];
     float m_run[TW], l_run[TW];
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
         m_run[t] = -INFINITY;
         l_run[t] = 0.f;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < X::DB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
     }
-    if (n_tiles > 0) fetch(0);
     for (int it = 0; it < n_tiles; ++it) {
-        const int kb = it * KT;
+        const int kb = (g.lo + wave + it * kPgWaves) * kNarrowTile;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < X::NLD; ++i) {
+                *reinterpret_cast<u32x4*>(kslab + (h * kPgGroup + i * X::RPI + v_row) * X::KSTRIDE + v_chunk * 16) = kst[h][i];
+                *reinterpret_cast<u32x4*>(vslab + (h * kPgGroup + i * X::RPI + v_row) * X::VSTRIDE + v_chunk * 16) = vst[h][i];
+            }
+        const int have = have_next;
+        if (it + 1 < n_tiles) fetch(it + 1);
+        const bool masked = have != 3 || kb + kNarrowTile > before + 1;
+        bf16x8 kf[X::KS], pf[TW][2];
+#pragma unroll
+        for (int s = 0; s < X::KS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(kslab + ln * X::KSTRIDE + (2 * s + hh) * 16);
+#pragma unroll
+        for (int t = 0; t < TW; ++t) {
+            if (t > 0 && !two) continue;
+            f32x16 s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < X::KS; ++k) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[t][k], s, 0, 0, 0);
+            softmax_step<X::DB>(s, oacc[t], m_run[t], l_run[t], pf[t], p.scale_log2, lim[t] - kb - hh * 4, have, masked);
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int db = 0; db < X::DB; ++db) {
+                const bf16x8 v = read_v<D>(vslab + tr_off + kk * 16 * X::VSTRIDE + db * 64);
+#pragma unroll
+                for (int t = 0; t < TW; ++t)
+                    if (t == 0 || two) oacc[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[t][kk], oacc[t][db], 0, 0, 0);
+            }
+    }
+    // the wavefronts' states of a row tile meet in LDS, in their order
+    const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
+    constexpr int F4 = D / 4, QPT = 32 * F4 / kPgThreads, RSTEP = kPgThreads / F4;
+    const int c4 = tid % F4, row0 = tid / F4;
+    float* obuf = reinterpret_cast<float*>(kslab);
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+        if (t > 0 && !two) continue;
+        if (t > 0) __syncthreads();  // the row tile before has been read
+        const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
+        if (hh == 0) {
+            sh_m[wave][ln] = m_run[t];
+            sh_l[wave][ln] = l;
+        }
+#pragma unroll
+        for (int db = 0; db < X::DB; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4*>(obuf + ln * X::OSTRIDE + db * 32 + q * 8 + hh * 4) =
+                    make_float4(oacc[t][db][q * 4], oacc[t][db][q * 4 + 1], oacc[t][db][q * 4 + 2], oacc[t][db][q * 4 + 3]);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < QPT; ++q) {
+            const int rt = row0 + q * RSTEP, r = t * 32 + rt;
+            if (r >= g.nrows) continue;
+            float M = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int v = 0; v < kPgWaves; ++v) M = fmaxf(M, sh_m[v][rt]);
+            const float Mu = M == -INFINITY ? 0.f : M;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int v = 0; v < kPgWaves; ++v) {
+                const float f = __builtin_amdgcn_exp2f(sh_m[v][rt] - Mu);
+                const float4 ov = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds + v * X::SLAB) + rt * X::OSTRIDE + c4 * 4);
+                sum += sh_l[v][rt] * f;
+                o.x += ov.x * f; o.y += ov.y * f; o.z += ov.z * f; o.w += ov.w * f;
+            }
+            if (g.parts == 1) {
+                store_out(p, g, r, c4, o, M, sum);
+            } else {
+                const unsigned at = (unsigned)part_slot(w, g.w0) * p.part_rows + r;
+                part_store4(rs, p.off_o + (at * D + c4 * 4) * 4u, o);
+                if (c4 == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(M, sum));
+            }
+        }
+    }
+    if (g.parts > 1) arrive<D>(p, g, rs, w, sh);
+    __syncthreads();  // the slabs are free
+}
+
+// A wide item's part: the workgroup loads a tile together, wavefront w takes rows w * TW * 32 on.
+template <int D>
+__device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, int* sh) {
+    using X = Tile<D>;
+    constexpr int TW = kWideRows / (kPgWaves * 32);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
+    const int ln = lane & 31, hh = lane >> 5;
+    const int32_t* row = p.table + g.b * p.table_stride;
+    unsigned char *kslab = lds, *vslab = lds + kWideTile * X::KSTRIDE;
+    const int before = g.L - g.n;  // row r of the stack sees the keys in front of before + r / G + 1
+    const int keys = max(0, before + quot(g.row0 + g.nrows - 1, p.d_g) + 1);
+    const int first_lim = before + quot(min(g.row0 + wave * TW * 32, g.row0 + g.nrows - 1), p.d_g) + 1;  // what all rows of the wavefront see
+    bf16x8 qf[TW][X::KS];
+    int lim[TW];
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+        const int r = min(g.row0 + (wave * TW + t) * 32 + ln, g.row0 + g.nrows - 1), i = quot(r, p.d_g);
+        lim[t] = before + i + 1;
+        const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
+#pragma unroll
+        for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
+    }
+    const bool busy = wave * TW * 32 < g.nrows;
+    const int v_row = lane / X::LPR, v_chunk = lane % X::LPR;
+    const int blk = lane >> 4, i16 = lane & 15;
+    const int tr_off = ((blk >> 1) * 4 + (i16 >> 2)) * X::VSTRIDE + ((blk & 1) * 16 + (i16 & 3) * 4) * 2;
+    int ahead = 0, ahead_have = 0, ahead_from = 0;  // the wavefront's own entry of a tile; which of its four groups have one
+    auto look_ahead = [&](int it) {
+        ahead_from = it;
+        ahead_have = 0;
+        const int kb = (it + lane) * kWideTile;
+#pragma unroll
+        for (int i = 0; i < kWideTile / kPgGroup; ++i) {
+            const int e = page_entry(p, row, kb + i * kPgGroup);
+            if ((unsigned)e < (unsigned)p.pages) ahead_have |= 1 << i;
+            if (i == wave) ahead = e;
+        }
+    };
+    u32x4 kst[X::NLD], vst[X::NLD];
+    int have_next = 0;
+    auto fetch = [&](int it) {
+        if (it - ahead_from >= kWave) look_ahead(it);
+        const int e = __builtin_amdgcn_readlane(ahead, it - ahead_from), key = it * kWideTile + wave * kPgGroup;
+        have_next = __builtin_amdgcn_readlane(ahead_have, it - ahead_from);
+        const unsigned bytes = group_bytes(p, e, key, keys, D * 2);
+        const long long at = group_at(p, e, key, g.kvh);
+        const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes), vr = buffer((const unsigned char*)p.V + at, bytes);
+#pragma unroll
+        for (int i = 0; i < X::NLD; ++i) {
+            const unsigned off = (unsigned)(i * X::RPI + v_row) * (unsigned)p.page_t + v_chunk * 16;
+            kst[i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (int)off, 0, 0);
+            vst[i] = __builtin_amdgcn_raw_buffer_load_b128(vr, (int)off, 0, 0);
+        }
+    };
+    f32x16 oacc[TW][X::DB];
+    float m_run[TW], l_run[TW];
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+        m_run[t] = -INFINITY;
+        l_run[t] = 0.f;
+#pragma unroll
+        for (int db = 0; db < X::DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
+    }
+    look_ahead(g.lo);
+    fetch(g.lo);
+    for (int it = g.lo; it < g.hi; ++it) {
+        const int kb = it * kWideTile;
         __syncthreads();  // the tile before has been read
 #pragma unroll
-        for (int i = 0; i < NLD; ++i) {
-            *reinterpret_cast<u32x4*>(kslab + (wave * kPgGroup + i * RPI + v_row) * KSTRIDE + v_chunk * 16) = kst[i];
-            *reinterpret_cast<u32x4*>(vslab + (wave * kPgGroup + i * RPI + v_row) * VSTRIDE + v_chunk * 16) = vst[i];
+        for (int i = 0; i < X::NLD; ++i) {
+            *reinterpret_cast<u32x4*>(kslab + (wave * kPgGroup + i * X::RPI + v_row) * X::KSTRIDE + v_chunk * 16) = kst[i];
+            *reinterpret_cast<u32x4*>(vslab + (wave * kPgGroup + i * X::RPI + v_row) * X::VSTRIDE + v_chunk * 16) = vst[i];
         }
-        have = have_next;
+        const int have = have_next;
         __syncthreads();
-        if (it + 1 < n_tiles) fetch(kb + KT);
+        if (it + 1 < g.hi) fetch(it + 1);
+        if (!busy) continue;
+        const bool masked = have != 15 || kb + kWideTile > first_lim;
 #pragma unroll
-        for (int half = 0; half < KT / 32; ++half) {
-            bf16x8 kf[KS];
+        for (int half = 0; half < kWideTile / 32; ++half) {
+            bf16x8 kf[X::KS], pf[TW][2];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(kslab + (half * 32 + ln) * KSTRIDE + (2 * s + hh) * 16);
-            bf16x8 pf[TW][2];
+            for (int s = 0; s < X::KS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(kslab + (half * 32 + ln) * X::KSTRIDE + (2 * s + hh) * 16);
 #pragma unroll
             for (int t = 0; t < TW; ++t) {
-                // S^T[key][row]; register i of this lane is key kb + half * 32 + (i / 4) * 8 + hh * 4 + i % 4 for row ln
-                f32x16 acc;
+                f32x16 s;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+                for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[t][s], acc, 0, 0, 0);
-                const int vis = lim[t] - (kb + half * 32) - hh * 4;
-                float mx = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float sc = acc[i] * p.scale_log2;
-                    sc = (i >> 2) * 8 + (i & 3) < vis && (have >> (half * 2 + (i >> 3)) & 1) ? sc : -INFINITY;
-                    acc[i] = sc;
-                    mx = fmaxf(mx, sc);
-                }
-                mx = fmaxf(mx, shfl_xor_f(mx, 32));
-                const float m_new = fmaxf(m_run[t], mx);
-                const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
-                const float alpha = __builtin_amdgcn_exp2f(m_run[t] - m_use);
-                float psum = 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float pv = __builtin_amdgcn_exp2f(acc[i] - m_use);
-                    psum += pv;
-                    pf[t][i >> 3][i & 7] = (__bf16)pv;
-                }
-                l_run[t] = l_run[t] * alpha + psum;
-                m_run[t] = m_new;
-                if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-                    for (int db = 0; db < DB; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) oacc[t][db][i] *= alpha;
-                }
+                for (int k = 0; k < X::KS; ++k) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[t][k], s, 0, 0, 0);
+                softmax_step<X::DB>(s, oacc[t], m_run[t], l_run[t], pf[t], p.scale_log2, lim[t] - (kb + half * 32) - hh * 4, have >> (half * 2), masked);
             }
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    union {
-                        short4v s[2];
-                        bf16x8 v;
-                    } vf;
-                    const unsigned char* ap = vslab + tr_off + (half * 32 + kk * 16) * VSTRIDE + db * 64;
-                    vf.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(ap));
-                    vf.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(ap + 8 * VSTRIDE));
+                for (int db = 0; db < X::DB; ++db) {
+                    const bf16x8 v = read_v<D>(vslab + tr_off + (half * 32 + kk * 16) * X::VSTRIDE + db * 64);
 #pragma unroll
-                    for (int t = 0; t < TW; ++t) oacc[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[t][kk], oacc[t][db], 0, 0, 0);
+                    for (int t = 0; t < TW; ++t) oacc[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[t][kk], oacc[t][db], 0, 0, 0);
                 }
         }
     }
+    const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
         const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
-        const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);  // a row that sees nothing is 0; NaN stays
-        const int r = row0 + (wave * TW + t) * 32 + ln;
-        if (r >= rows) continue;
-        const int i = quot(r, p.d_g), h = kvh * p.G + r - i * p.G;
-        unsigned char* op = (unsigned char*)p.O + (br.first + i) * p.o_t + h * p.o_h;
+        const int r = (wave * TW + t) * 32 + ln;
+        if (r >= g.nrows) continue;
+        const unsigned at = (unsigned)part_slot(w, g.w0) * p.part_rows + r;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < X::DB; ++db)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                bf16x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oacc[t][db][q * 4 + e] * inv);
-                *reinterpret_cast<bf16x4*>(op + (db * 32 + q * 8 + hh * 4) * 2) = v;
+                const int c4 = db * 8 + q * 2 + hh;
+                const float4 o = make_float4(oacc[t][db][q * 4], oacc[t][db][q * 4 + 1], oacc[t][db][q * 4 + 2], oacc[t][db][q * 4 + 3]);
+                if (g.parts == 1) store_out(p, g, r, c4, o, m_run[t], l);
+                else part_store4(rs, p.off_o + (at * D + c4 * 4) * 4u, o);
             }
-        if (p.lse && hh == 0) p.lse[(long long)(br.first + i) * p.Hq + h] = (m_run[t] + log2f(l)) * 0.69314718055994530942f;
+        if (g.parts > 1 && hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run[t], l));
+    }
+    if (g.parts > 1) arrive<D>(p, g, rs, w, sh);
+    __syncthreads();
+}
+
+template <int D, int NARROW_TILES, bool WIDE>
+__global__ __launch_bounds__(kPgThreads, !WIDE && NARROW_TILES == 1 ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
+    __shared__ __attribute__((aligned(16))) unsigned char lds[Tile<D>::LDS];
+    __shared__ float sh_m[kPgWaves][32], sh_l[kPgWaves][32];
+    __shared__ int sh;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int per_xcd = p.workers / kNumXCD;  // neighbours in the sequence share an XCD and with it a KV head's keys in its L2
+    const int w = (int)(blockIdx.x % kNumXCD) * per_xcd + (int)(blockIdx.x / kNumXCD);
+    int base = 0;
+    Items items = items_at<WIDE, NARROW_TILES>(p, 0, 0, lane);
+    unsigned total = __builtin_amdgcn_readlane(items.end, kWave - 1);
+    for (int s = kWave; s < p.items; s += kWave) total = __builtin_amdgcn_readlane(items_at<WIDE, NARROW_TILES>(p, s, total, lane).end, kWave - 1);
+    if (total == 0) return;
+    Pieces pieces;
+    pieces.places = (double)total * p.Hkv;
+    pieces.workers = (int)fmin((double)p.workers, fmax(1.0, pieces.places / kMinPiece));
+    if (w >= pieces.workers) return;
+    long long at = pieces.start(w);
+    const long long end = pieces.start(w + 1);
+    int kvh = (int)(at / total);
+    unsigned within = (unsigned)(at - (long long)kvh * total);
+    while (at < end) {
+        // the item that has place `within`
+        while ((unsigned)__builtin_amdgcn_readlane(items.end, kWave - 1) <= within) {
+            base += kWave;
+            items = items_at<WIDE, NARROW_TILES>(p, base, __builtin_amdgcn_readlane(items.end, kWave - 1), lane);
+        }
+        const int i = __builtin_ctzll(__ballot(items.end > within));
+        Segment g;
+        g.b = __builtin_amdgcn_readlane(items.b, i);
+        g.kvh = kvh;
+        g.first = __builtin_amdgcn_readlane(items.first, i);
+        g.n = __builtin_amdgcn_readlane(items.n, i);
+        g.L = __builtin_amdgcn_readlane(items.L, i);
+        g.row0 = __builtin_amdgcn_readlane(items.row0, i);
+        g.tiles = __builtin_amdgcn_readlane(items.tiles, i);
+        const unsigned item_end = __builtin_amdgcn_readlane(items.end, i);
+        const int cost = __builtin_amdgcn_readlane(items.cost, i), rows = g.n * p.G;
+        const bool narrow = !WIDE || rows <= NARROW_TILES * 32;
+        if (narrow) g.row0 = 0;
+        g.nrows = min(p.part_rows, narrow ? rows : min(kWideRows, rows - g.row0));  // (what max_new allows)
+        const int each = narrow ? kNarrowCost : kWideCost;
+        const long long head = (long long)kvh * total, tile0 = head + item_end - cost + kStartCost;
+        auto tile_from = [&](long long place) { return place <= tile0 ? 0 : (int)min((long long)g.tiles, (place - tile0 + each - 1) / each); };
+        g.lo = tile_from(at);
+        g.hi = tile_from(end);
+        if (g.lo < g.hi) {
+            g.w0 = w;
+            g.parts = 1;
+            if (g.lo > 0 || g.hi < g.tiles) {
+                g.w0 = g.lo > 0 ? pieces.worker(tile0) : w;
+                g.parts = (g.hi < g.tiles ? pieces.worker(tile0 + (long long)(g.tiles - 1) * each) : w) - g.w0 + 1;
+            }
+            if (narrow) narrow_segment<D, NARROW_TILES>(p, g, w, lds, sh_m, sh_l, &sh);
+            else if (WIDE) wide_segment<D>(p, g, w, lds, &sh);
+        }
+        within = item_end;
+        at = head + within;
+        if (within >= total) {
+            ++kvh;
+            within = 0;
+            if (base > 0) items = items_at<WIDE, NARROW_TILES>(p, base = 0, 0, lane);
+        }
     }
 }
 
@@ -383,8 +814,35 @@ static int paged_desc(const lotts_paged_desc* in, bool uniform, lotts_paged_desc
         if (s < 0 || (s * es) % 16 != 0) return LOTTS_ERR_SHAPE;
     if (d->q_stride_h < D || d->o_stride_h < D || d->page_stride_t < D || d->table_stride < d->columns) return LOTTS_ERR_SHAPE;
     if (d->page_stride_t * es > (1LL << 26)) return LOTTS_ERR_SHAPE;  // 16 keys of a page: 32-bit offsets
+    // the sequence of work of a KV head in 32 bits (were every branch as long as the table allows)
+    const long long G = d->Hq / d->Hkv, slots = (long long)d->T * G / kWideRows + d->B;
+    if (((long long)d->columns << *shift) / kNarrowTile * kNarrowCost + kWideCost + kStartCost > 0x7fffffffLL / slots) return LOTTS_ERR_SHAPE;
     if ((long long)d->T * d->Hq >= (1LL << 24)) return LOTTS_ERR_SHAPE;  // a grid holds fewer than 2^24 workgroups of 256 threads
     return LOTTS_OK;
+}
+
+constexpr int kPgTagShift = 16;
+static std::atomic<unsigned long long> g_paged_tag{0};
+
+// Which kernel, how many workers, and where the partials lie: [arrival cells][(maximum, sum)][outputs].
+struct PagedPlan {
+    bool wide;
+    int narrow_tiles, workers, items, part_rows;
+    size_t off_ml, off_o, bytes;
+};
+static PagedPlan paged_plan(const lotts_paged_desc& d) {
+    PagedPlan pl = {};
+    const long long G = d.Hq / d.Hkv, rows = d.max_new * G;
+    pl.wide = rows > 64;
+    pl.narrow_tiles = rows > 32 ? 2 : 1;
+    pl.workers = kNumCU;
+    pl.items = (int)(pl.wide ? d.T * G / kWideRows + d.B : d.B);
+    pl.part_rows = (int)std::min<long long>(kWideRows, (rows + 7) / 8 * 8);
+    const size_t slots = 2 * (size_t)pl.workers;
+    pl.off_ml = 4 * (size_t)pl.workers * sizeof(unsigned long long);
+    pl.off_o = pl.off_ml + slots * pl.part_rows * 8;
+    pl.bytes = pl.off_o + slots * pl.part_rows * d.D * 4;
+    return pl;
 }
 
 }  // namespace lotts
@@ -394,7 +852,7 @@ extern "C" size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc*
     lotts_paged_desc d;
     int shift;
     if (paged_desc(desc, false, &d, &shift) != LOTTS_OK) return 0;
-    return 256;
+    return d.dtype == LOTTS_F32 ? 256 : paged_plan(d).bytes;
 }
 
 extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* Q, const void* Kpages, const void* Vpages, const int32_t* page_table,
@@ -408,7 +866,8 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     if (!Q || !Kpages || !Vpages || !page_table || !kv_len || !O || !workspace) return LOTTS_ERR_NULL;
     if ((((uintptr_t)Q | (uintptr_t)Kpages | (uintptr_t)Vpages | (uintptr_t)O | (uintptr_t)workspace) & 15) != 0) return LOTTS_ERR_SHAPE;
     if ((((uintptr_t)page_table | (uintptr_t)kv_len | (uintptr_t)q_start | (uintptr_t)lse) & 3) != 0) return LOTTS_ERR_SHAPE;
-    if (workspace_bytes < verify_attention_paged_workspace_bytes(desc)) return LOTTS_ERR_WORKSPACE;
+    const PagedPlan pl = paged_plan(d);
+    if (workspace_bytes < (d.dtype == LOTTS_F32 ? 256 : pl.bytes)) return LOTTS_ERR_WORKSPACE;
     const long long es = d.dtype == LOTTS_BF16 ? 2 : 4;
     PagedParams p;
     p.Q = Q; p.K = Kpages; p.V = Vpages; p.table = page_table; p.kv_len = kv_len; p.q_start = q_start; p.O = O; p.lse = lse;
@@ -419,20 +878,29 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     p.pages = d.pages; p.columns = d.columns; p.shift = shift;
     const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.D);
     p.scale_log2 = (float)(scale * 1.4426950408889634074);
-    p.d_hkv = fast_div(d.Hkv); p.d_g = fast_div(p.G);
-    p.tiles = 0;
+    p.d_g = fast_div(p.G);
+    p.items = pl.items; p.workers = pl.workers; p.part_rows = pl.part_rows;
+    p.ws = workspace; p.ws_bytes = (unsigned)pl.bytes; p.off_ml = (unsigned)pl.off_ml; p.off_o = (unsigned)pl.off_o;
+    p.cells = static_cast<unsigned long long*>(workspace);
+    p.tag = (g_paged_tag.fetch_add(1, std::memory_order_relaxed) + 1) << kPgTagShift;
     const hipStream_t s = (hipStream_t)stream;
+    const dim3 block(kPgThreads);
     if (d.dtype == LOTTS_F32) {
         const dim3 grid((unsigned)((long long)d.T * d.Hq));
-        if (d.D == 64) LOTTS_LAUNCH(paged_f32_kernel<64>, grid, dim3(kPgThreads), s, p);
-        else LOTTS_LAUNCH(paged_f32_kernel<128>, grid, dim3(kPgThreads), s, p);
+        if (d.D == 64) LOTTS_LAUNCH(paged_f32_kernel<64>, grid, block, s, p);
+        else LOTTS_LAUNCH(paged_f32_kernel<128>, grid, block, s, p);
         return check_launch();
     }
-    constexpr int TW = 1, rows = kPgWaves * TW * 32;
-    p.tiles = (int)((long long)d.T * p.G / rows) + d.B;
-    const long long items = (long long)p.tiles * d.Hkv;
-    if (items >= (1LL << 24)) return LOTTS_ERR_SHAPE;
-    if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, TW>), dim3((unsigned)items), dim3(kPgThreads), s, p);
-    else LOTTS_LAUNCH((paged_attn_kernel<128, TW>), dim3((unsigned)items), dim3(kPgThreads), s, p);
+    const dim3 grid((unsigned)pl.workers);
+    if (pl.wide) {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, true>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 2, true>), grid, block, s, p);
+    } else if (pl.narrow_tiles == 2) {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, false>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 2, false>), grid, block, s, p);
+    } else {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, false>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, false>), grid, block, s, p);
+    }
     return check_launch();
 }

@@ -259,7 +259,7 @@ def test_a_generation(lotts, captured):
         lotts.kv_append_paged(qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], pool[0], pool[1], table, kv_len, q_start)
         lotts.verify_attention_paged(qkv[:, :Hq], pool[0], pool[1], table, kv_len, q_start, out=out, lse=lse, workspace=attn_ws)
 
-    attn_ws = torch.zeros(32 << 20, dtype=torch.uint8, device=DEV)
+    attn_ws = torch.zeros(256 << 20, dtype=torch.uint8, device=DEV)
     graph = None
     if captured:
         enqueue()   # with no new tokens: nothing changes

@@ -132,7 +132,7 @@ def test_a_cache_beyond_4_gib(lotts):
 def test_replays(lotts):
     """Captured once, replayed with other lengths, other pages and other numbers of new tokens."""
     first = Cache([2, 30, 1], [100, 64, 257], 16, 2, 128, 16, seed=0, spare_pages=40, more_columns=30)
-    ws = torch.zeros(64 << 20, dtype=torch.uint8, device=DEV)
+    ws = torch.zeros(256 << 20, dtype=torch.uint8, device=DEV)
     out = torch.zeros_like(first.Q)
     lse = torch.zeros(first.q.shape[:2], device=DEV)
     call = lambda: lotts.verify_attention_paged(first.Q, first.K, first.V, first.table, first.kv_len, first.q_start, out=out, lse=lse, max_new=32,
