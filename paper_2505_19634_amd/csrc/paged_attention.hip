@@ -16,6 +16,8 @@ namespace lotts {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
@@ -289,30 +291,32 @@ struct Tile {
     static constexpr int SLAB = kNarrowTile * (KSTRIDE + VSTRIDE);  // LDS of a wavefront (narrow)
     static constexpr int LDS = kPgWaves * SLAB;
     static_assert(32 * OSTRIDE * 4 <= SLAB, "a parked output reuses the wavefront's slab");
-    static_assert(kWideTile * (KSTRIDE + VSTRIDE) <= LDS, "a wide tile fits");
 };
 
-// One row tile's step: scores of 32 keys, mask, running maximum and sum; the weights come back in the order in which the product with V takes
-// them.  Register i of a lane is key (i / 4) * 8 + hh * 4 + i % 4 of the tile, for row `lane % 32`; vis: keys in front of it are seen;
-// have: bit g: 16 keys from 16 g on lie in a page.
+// Maximum of a lane's and its partner's 32 lanes away.
+__device__ __forceinline__ float max_halves(float v) {
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// One row tile's step: scores of 32 keys, mask, running maximum (of the products as they are; the scale comes with the exponential) and
+// sum; the weights come back in the order in which the product with V takes them.  Register i of a lane is key (i / 4) * 8 + hh * 4 + i % 4 of
+// the tile, for row `lane % 32`; vis: keys in front of it are seen; have: bit g: 16 keys from 16 g on lie in a page.
 template <int DB>
 __device__ __forceinline__ void softmax_step(f32x16& s, f32x16 (&o)[DB], float& m, float& l, bf16x8 (&pf)[2], float scale, int vis, int have, bool masked) {
-    float mx = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] *= scale;
     if (masked) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (i >> 2) * 8 + (i & 3) < vis && (have >> (i >> 3) & 1) ? s[i] : -INFINITY;
     }
+    float mx = m;
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    mx = fmaxf(mx, shfl_xor_f(mx, 32));
-    const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+    const float m_new = max_halves(mx), m_use = m_new == -INFINITY ? 0.f : m_new * scale;
+    const float alpha = __builtin_amdgcn_exp2f(m * scale - m_use);
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const float w = __builtin_amdgcn_exp2f(s[i] - m_use);
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m_use));
         sum += w;
         pf[i >> 3][i & 7] = (__bf16)w;  // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
     }
@@ -448,7 +452,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
         if (t > 0) __syncthreads();  // the row tile before has been read
         const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
         if (hh == 0) {
-            sh_m[wave][ln] = m_run[t];
+            sh_m[wave][ln] = m_run[t] * p.scale_log2;
             sh_l[wave][ln] = l;
         }
 #pragma unroll
@@ -487,32 +491,220 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
     __syncthreads();  // the slabs are free
 }
 
-// A wide item's part: the workgroup loads a tile together, wavefront w takes rows w * TW * 32 on.
+// ---- wide items ----
+// A stage of LDS holds the K and V rows of a tile, 16 bytes a piece, put there by the loads themselves: lane i of a load writes piece i behind
+// the load's base, so rows cannot be padded; instead piece c of row r lies at c ^ spread(r), which the lane that loads it picks.  Both the 16-byte row
+// reads of K (32 rows, one piece) and the transposing reads of V (8 rows, 4 neighbouring pieces) then meet every bank equally often.
+template <int D>
+__device__ __forceinline__ int spread(int r) {
+    if (D == 128) return (r & 3) << 2 | (r >> 2 & 3);  // 16 pieces a row
+    return (r >> 1 & 1) << 2 | (r >> 2 & 3);           // 8 pieces a row, two rows next to each other
+}
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // M0 is on the clobber list on purpose
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned off, unsigned lds_base) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(off), "s"(lds_base), "s"(r) : "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ unsigned lds_address(const void* at) {
+    return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)at);
+}
+
+constexpr int kStages = 4;     // tiles in LDS: one whose V is read, one whose K is read, two on their way
+constexpr float kRescale = 8.f;  // a running maximum may be behind the true one by a factor of 2^8 before the state is rescaled
+
+// The products of a wide item are written as instructions, so that every operand lies where it should: outputs and Q in accumulation registers,
+// scores where the vector units reach them.  (Left to choose, the compiler put the scores into accumulation registers too, Q into scratch memory
+// and the waits for that into the loop.)  It does not know how long these take: what reads a result on the vector units is kept behind
+// two later products, or behind mfma_done().
+__device__ __forceinline__ void mfma_first(f32x16& d, const bf16x8& a, const bf16x8& b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "a"(b));
+}
+__device__ __forceinline__ void mfma_scores(f32x16& d, const bf16x8& a, const bf16x8& b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "a"(b));
+}
+__device__ __forceinline__ void mfma_output(f32x16& d, const bf16x8& a, const bf16x8& b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_done() { asm volatile("s_nop 15\n\ts_nop 15"); }
+
+// The loop over a wide item's tiles for a wavefront with N row tiles.  next(j) brings tile j in: it waits for its loads and for the other wavefronts,
+// and requests one more.  While the matrix cores multiply K of tile j + 1 with Q, the vector units turn the scores of tile j into weights; then V of
+// tile j is multiplied while the scores of tile j + 1 are scaled and their maximum is taken.  A wavefront has its SIMD to itself and issues in
+// order, so the two streams are written down interleaved, a pair of products and its share of the vector work at a time, and the
+// scheduling barriers keep them so.
+template <int D, int N, typename Next>
+__device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const unsigned char* lds, const bf16x8 (&qf)[2][Tile<D>::KS], const int (&lim)[2],
+                                          int first_lim, const int (&kat)[Tile<D>::KS], const int (&vat)[Tile<D>::DB][2], f32x16 (&o)[2][Tile<D>::DB],
+                                          float (&m)[2], float (&l)[2], Next next) {
+    using X = Tile<D>;
+    constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
+    constexpr int QG = X::KS, VG = 2 * X::DB;   // groups of products with 32 keys of K and of V, N products each
+    constexpr int QE = 16 / QG, VE = 16 / VG;   // scores of a row tile that a group takes care of
+    constexpr int AHEAD = 3;                    // groups between a read from LDS and its use
+    constexpr int WAIT = 3 - N;                 // groups with V, N products each, in front of the first look at the scores
+    float s[N][16], m_use[N], mx[N];
+    f32x16 n[N];
+    bf16x8 pf[N][2];
+    const float scale = p.scale_log2;
+    auto read_k = [&](const unsigned char* st, int i) { return *reinterpret_cast<const bf16x8*>(st + kat[i]); };
+    auto read_v = [&](const unsigned char* st, int i) {
+        union {
+            short4v s[2];
+            bf16x8 v;
+        } f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(st + (i / X::DB) * 16 * ROW + vat[i % X::DB][h]));
+        return f.v;
+    };
+    auto weigh = [&](int i) {  // scores of group i: weights, their sums
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+#pragma unroll
+            for (int e = 0; e < QE; ++e) {
+                const int x = i * QE + e;
+                s[t][x] = __builtin_amdgcn_exp2f(s[t][x] - m_use[t]);
+                l[t] += s[t][x];
+            }
+            // (pinned where they are computed: the compiler would move them down to the products that use them, behind the mask's branch)
+            asm volatile("" : "+v"(l[t]));
+#pragma unroll
+            for (int e = 0; e < QE; e += 2) {
+                const int x = i * QE + e;
+                u32x4 all = __builtin_bit_cast(u32x4, pf[t][x >> 3]);
+                // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
+                const f32x2 pair = {s[t][x], s[t][x + 1]};
+                unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, bf16x2));
+                asm volatile("" : "+v"(u));
+                all[(x & 7) >> 1] = u;
+                pf[t][x >> 3] = __builtin_bit_cast(bf16x8, all);
+            }
+        }
+    };
+    auto take = [&](int i) {  // scores of group i of the next 32 keys: scaled, maximum
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const int x = i * VE + e;
+                s[t][x] = n[t][x] * scale;
+                mx[t] = fmaxf(mx[t], s[t][x]);
+            }
+    };
+    auto mask = [&](int kb, int have) {
+        if ((have & 3) == 3 && kb + 32 <= first_lim) return;
+        mfma_done();
+        const int hh = (threadIdx.x & 32) >> 5;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int vis = lim[t] - kb - hh * 4;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) n[t][x] = (x >> 2) * 8 + (x & 3) < vis && (have >> (x >> 3) & 1) ? n[t][x] : -INFINITY;
+        }
+    };
+    auto settle = [&] {  // the running maximum of the scores in s; o and l follow where it has risen much
+        bool rise[N], any = false;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            mx[t] = max_halves(mx[t]);
+            rise[t] = mx[t] > m[t] + kRescale;
+            any = any || rise[t];
+        }
+        if (__builtin_amdgcn_ballot_w64(any) != 0) {
+            mfma_done();
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const float m_new = rise[t] ? mx[t] : m[t], base = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = __builtin_amdgcn_exp2f(m[t] - base);
+                m[t] = m_new;
+                m_use[t] = base;
+                l[t] *= alpha;
+#pragma unroll
+                for (int db = 0; db < X::DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[t][db][i] *= alpha;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < N; ++t) mx[t] = -INFINITY;
+    };
+    auto multiply_k = [&](int i, const bf16x8& k) {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            if (i == 0) mfma_first(n[t], k, qf[t][i]);
+            else mfma_scores(n[t], k, qf[t][i]);
+        }
+    };
+    auto multiply_v = [&](int i, const bf16x8& v) {
+#pragma unroll
+        for (int t = 0; t < N; ++t) mfma_output(o[t][i % X::DB], v, pf[t][i / X::DB]);
+    };
+    // 32 keys are weighed and multiplied with V (at vst) while the next 32, at kst, key kb on, are multiplied with Q
+    auto step = [&](const unsigned char* vst, const unsigned char* kst, int kb, int have) {
+        bf16x8 f[QG + VG];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) f[i] = read_k(kst, i);
+#pragma unroll
+        for (int i = 0; i < QG; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            f[i + AHEAD] = i + AHEAD < QG ? read_k(kst, i + AHEAD) : read_v(vst, i + AHEAD - QG);
+            multiply_k(i, f[i]);
+            weigh(i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        mask(kb, have);
+#pragma unroll
+        for (int i = 0; i < VG; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + AHEAD < VG) f[QG + i + AHEAD] = read_v(vst, i + AHEAD);
+            multiply_v(i, f[QG + i]);
+            if (i >= WAIT) take(i - WAIT);
+        }
+#pragma unroll
+        for (int i = VG - WAIT; i < VG; ++i) take(i);
+        __builtin_amdgcn_sched_barrier(0);
+        settle();
+    };
+#pragma unroll
+    for (int t = 0; t < N; ++t) m_use[t] = 0.f, mx[t] = -INFINITY;
+    int have = next(lo);
+    const unsigned char* st = lds + (lo % kStages) * STAGE;
+#pragma unroll
+    for (int i = 0; i < QG; ++i) multiply_k(i, read_k(st, i));
+    mfma_done();
+    mask(lo * kWideTile, have);
+#pragma unroll
+    for (int i = 0; i < VG; ++i) take(i);
+    settle();
+    for (int it = lo; it < hi; ++it) {
+        step(st, st + 32 * ROW, it * kWideTile + 32, have >> 2);
+        if (it + 1 == hi) break;
+        have = next(it + 1);
+        const unsigned char* after = lds + ((it + 1) % kStages) * STAGE;
+        step(st + 32 * ROW, after, (it + 1) * kWideTile, have);
+        st = after;
+    }
+#pragma unroll
+    for (int i = 0; i < QG; ++i) weigh(i);
+#pragma unroll
+    for (int i = 0; i < VG; ++i) multiply_v(i, read_v(st + 32 * ROW, i));
+    mfma_done();
+}
+
+// The workgroup loads a tile together, 16 keys a wavefront; wavefront w takes the row tiles w and w + 4 of the item.
 template <int D>
 __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, int* sh) {
     using X = Tile<D>;
     constexpr int TW = kWideRows / (kPgWaves * 32);
+    constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;  // bytes
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     const int ln = lane & 31, hh = lane >> 5;
     const int32_t* row = p.table + g.b * p.table_stride;
-    unsigned char *kslab = lds, *vslab = lds + kWideTile * X::KSTRIDE;
     const int before = g.L - g.n;  // row r of the stack sees the keys in front of before + r / G + 1
     const int keys = max(0, before + quot(g.row0 + g.nrows - 1, p.d_g) + 1);
-    const int first_lim = before + quot(min(g.row0 + wave * TW * 32, g.row0 + g.nrows - 1), p.d_g) + 1;  // what all rows of the wavefront see
-    bf16x8 qf[TW][X::KS];
-    int lim[TW];
-#pragma unroll
-    for (int t = 0; t < TW; ++t) {
-        const int r = min(g.row0 + (wave * TW + t) * 32 + ln, g.row0 + g.nrows - 1), i = quot(r, p.d_g);
-        lim[t] = before + i + 1;
-        const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
-#pragma unroll
-        for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
-    }
-    const bool busy = wave * TW * 32 < g.nrows;
-    const int v_row = lane / X::LPR, v_chunk = lane % X::LPR;
-    const int blk = lane >> 4, i16 = lane & 15;
-    const int tr_off = ((blk >> 1) * 4 + (i16 >> 2)) * X::VSTRIDE + ((blk & 1) * 16 + (i16 & 3) * 4) * 2;
+    const int first_lim = before + quot(min(g.row0 + wave * 32, g.row0 + g.nrows - 1), p.d_g) + 1;  // what all rows of the wavefront see
+    const int v_row = lane / X::LPR, v_slot = lane % X::LPR;
     int ahead = 0, ahead_have = 0, ahead_from = 0;  // the wavefront's own entry of a tile; which of its four groups have one
     auto look_ahead = [&](int it) {
         ahead_from = it;
@@ -525,22 +717,61 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
             if (i == wave) ahead = e;
         }
     };
-    u32x4 kst[X::NLD], vst[X::NLD];
-    int have_next = 0;
+    unsigned src[X::NLD];
+#pragma unroll
+    for (int i = 0; i < X::NLD; ++i) {
+        const int r = i * X::RPI + v_row;
+        src[i] = (unsigned)r * (unsigned)p.page_t + (v_slot ^ spread<D>(r)) * 16;
+    }
+    const unsigned to = lds_address(lds) + wave * kPgGroup * ROW;
+    int have_1 = 0, have_2 = 0;  // of the next two tiles
     auto fetch = [&](int it) {
         if (it - ahead_from >= kWave) look_ahead(it);
         const int e = __builtin_amdgcn_readlane(ahead, it - ahead_from), key = it * kWideTile + wave * kPgGroup;
-        have_next = __builtin_amdgcn_readlane(ahead_have, it - ahead_from);
         const unsigned bytes = group_bytes(p, e, key, keys, D * 2);
         const long long at = group_at(p, e, key, g.kvh);
         const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes), vr = buffer((const unsigned char*)p.V + at, bytes);
+        const unsigned stage = to + it % kStages * STAGE;
 #pragma unroll
         for (int i = 0; i < X::NLD; ++i) {
-            const unsigned off = (unsigned)(i * X::RPI + v_row) * (unsigned)p.page_t + v_chunk * 16;
-            kst[i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (int)off, 0, 0);
-            vst[i] = __builtin_amdgcn_raw_buffer_load_b128(vr, (int)off, 0, 0);
+            load_to_lds(kr, src[i], stage + i * 1024);
+            load_to_lds(vr, src[i], stage + HALF + i * 1024);
         }
+        return __builtin_amdgcn_readlane(ahead_have, it - ahead_from);
     };
+    look_ahead(g.lo);
+    have_1 = fetch(g.lo);
+    if (g.lo + 1 < g.hi) have_2 = fetch(g.lo + 1);
+    // Tile j is in LDS for everybody; everybody has left tile j - 2 behind, whose stage the next request takes.
+    auto next = [&](int j) {
+        if (j + 1 < g.hi) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * X::NLD) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int have = have_1;
+        have_1 = have_2;
+        if (j + 2 < g.hi) have_2 = fetch(j + 2);
+        return have;
+    };
+    bf16x8 qf[TW][X::KS];
+    int lim[TW];
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+        const int r = min(g.row0 + (wave + t * kPgWaves) * 32 + ln, g.row0 + g.nrows - 1), i = quot(r, p.d_g);
+        lim[t] = before + i + 1;
+        const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
+#pragma unroll
+        for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
+    }
+    // where the lane finds its pieces in a stage
+    const int blk = lane >> 4, i16 = lane & 15;
+    int kat[X::KS], vat[X::DB][2];
+#pragma unroll
+    for (int s = 0; s < X::KS; ++s) kat[s] = ln * ROW + ((2 * s + hh) ^ spread<D>(ln & 15)) * 16;
+    const int vr = (blk >> 1) * 4 + (i16 >> 2);
+#pragma unroll
+    for (int db = 0; db < X::DB; ++db)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            vat[db][h] = HALF + (vr + h * 8) * ROW + ((db * 4 + (blk & 1) * 2 + (i16 >> 1 & 1)) ^ spread<D>(vr + h * 8)) * 16 + (i16 & 1) * 8;
     f32x16 oacc[TW][X::DB];
     float m_run[TW], l_run[TW];
 #pragma unroll
@@ -552,62 +783,44 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 #pragma unroll
             for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
     }
-    look_ahead(g.lo);
-    fetch(g.lo);
-    for (int it = g.lo; it < g.hi; ++it) {
-        const int kb = it * kWideTile;
-        __syncthreads();  // the tile before has been read
-#pragma unroll
-        for (int i = 0; i < X::NLD; ++i) {
-            *reinterpret_cast<u32x4*>(kslab + (wave * kPgGroup + i * X::RPI + v_row) * X::KSTRIDE + v_chunk * 16) = kst[i];
-            *reinterpret_cast<u32x4*>(vslab + (wave * kPgGroup + i * X::RPI + v_row) * X::VSTRIDE + v_chunk * 16) = vst[i];
-        }
-        const int have = have_next;
-        __syncthreads();
-        if (it + 1 < g.hi) fetch(it + 1);
-        if (!busy) continue;
-        const bool masked = have != 15 || kb + kWideTile > first_lim;
-#pragma unroll
-        for (int half = 0; half < kWideTile / 32; ++half) {
-            bf16x8 kf[X::KS], pf[TW][2];
-#pragma unroll
-            for (int s = 0; s < X::KS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(kslab + (half * 32 + ln) * X::KSTRIDE + (2 * s + hh) * 16);
-#pragma unroll
-            for (int t = 0; t < TW; ++t) {
-                f32x16 s;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-                for (int k = 0; k < X::KS; ++k) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], qf[t][k], s, 0, 0, 0);
-                softmax_step<X::DB>(s, oacc[t], m_run[t], l_run[t], pf[t], p.scale_log2, lim[t] - (kb + half * 32) - hh * 4, have >> (half * 2), masked);
-            }
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int db = 0; db < X::DB; ++db) {
-                    const bf16x8 v = read_v<D>(vslab + tr_off + (half * 32 + kk * 16) * X::VSTRIDE + db * 64);
-#pragma unroll
-                    for (int t = 0; t < TW; ++t) oacc[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[t][kk], oacc[t][db], 0, 0, 0);
-                }
-        }
+    const int row_tiles = __builtin_amdgcn_readfirstlane((g.nrows + 31) / 32 - wave);  // from this wavefront's first on
+    if (row_tiles > kPgWaves) {
+        wide_rows<D, 2>(p, g.lo, g.hi, lds, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
+    } else if (row_tiles > 0) {
+        wide_rows<D, 1>(p, g.lo, g.hi, lds, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
+    } else {
+        for (int j = g.lo; j < g.hi; ++j) next(j);
     }
     const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
         const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
-        const int r = (wave * TW + t) * 32 + ln;
+        const int r = (wave + t * kPgWaves) * 32 + ln;
         if (r >= g.nrows) continue;
         const unsigned at = (unsigned)part_slot(w, g.w0) * p.part_rows + r;
+        if (g.parts > 1) {
+#pragma unroll
+            for (int db = 0; db < X::DB; ++db)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    part_store4(rs, p.off_o + (at * D + db * 32 + q * 8 + hh * 4) * 4u,
+                                make_float4(oacc[t][db][q * 4], oacc[t][db][q * 4 + 1], oacc[t][db][q * 4 + 2], oacc[t][db][q * 4 + 3]));
+            if (hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run[t], l));
+            continue;
+        }
+        const int i = quot(g.row0 + r, p.d_g), h = g.kvh * p.G + g.row0 + r - i * p.G;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing is 0
+        unsigned char* op = (unsigned char*)p.O + (long long)(g.first + i) * p.o_t + h * p.o_h;
 #pragma unroll
         for (int db = 0; db < X::DB; ++db)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int c4 = db * 8 + q * 2 + hh;
-                const float4 o = make_float4(oacc[t][db][q * 4], oacc[t][db][q * 4 + 1], oacc[t][db][q * 4 + 2], oacc[t][db][q * 4 + 3]);
-                if (g.parts == 1) store_out(p, g, r, c4, o, m_run[t], l);
-                else part_store4(rs, p.off_o + (at * D + c4 * 4) * 4u, o);
+                bf16x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oacc[t][db][q * 4 + e] * inv);
+                *reinterpret_cast<bf16x4*>(op + (db * 32 + q * 8 + hh * 4) * 2) = v;
             }
-        if (g.parts > 1 && hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run[t], l));
+        if (p.lse && hh == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (m_run[t] + log2f(l)) * 0.69314718055994530942f;
     }
     if (g.parts > 1) arrive<D>(p, g, rs, w, sh);
     __syncthreads();
@@ -615,7 +828,8 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 
 template <int D, int NARROW_TILES, bool WIDE>
 __global__ __launch_bounds__(kPgThreads, !WIDE && NARROW_TILES == 1 ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
-    __shared__ __attribute__((aligned(16))) unsigned char lds[Tile<D>::LDS];
+    constexpr int WIDE_LDS = kStages * kWideTile * 2 * D * 2;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[WIDE && WIDE_LDS > Tile<D>::LDS ? WIDE_LDS : Tile<D>::LDS];
     __shared__ float sh_m[kPgWaves][32], sh_l[kPgWaves][32];
     __shared__ int sh;
     const int lane = threadIdx.x & (kWave - 1);
@@ -893,8 +1107,8 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     }
     const dim3 grid((unsigned)pl.workers);
     if (pl.wide) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, true>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 2, true>), grid, block, s, p);
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, true>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, true>), grid, block, s, p);
     } else if (pl.narrow_tiles == 2) {
         if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, false>), grid, block, s, p);
         else LOTTS_LAUNCH((paged_attn_kernel<128, 2, false>), grid, block, s, p);
