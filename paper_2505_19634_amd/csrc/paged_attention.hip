@@ -534,9 +534,8 @@ __device__ __forceinline__ void mfma_done() { asm volatile("s_nop 15\n\ts_nop 15
 // order, so the two streams are written down interleaved, a pair of products and its share of the vector work at a time, and the
 // scheduling barriers keep them so.
 template <int D, int N, typename Next>
-__device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const unsigned char* lds, const bf16x8 (&qf)[2][Tile<D>::KS], const int (&lim)[2],
-                                          int first_lim, const int (&kat)[Tile<D>::KS], const int (&vat)[Tile<D>::DB][2], f32x16 (&o)[2][Tile<D>::DB],
-                                          float (&m)[2], float (&l)[2], Next next) {
+__device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[2][Tile<D>::KS], const int (&lim)[2],
+                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[2][Tile<D>::DB], float (&m)[2], float (&l)[2], Next next) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
     constexpr int QG = X::KS, VG = 2 * X::DB;   // groups of products with 32 keys of K and of V, N products each
@@ -547,15 +546,17 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     f32x16 n[N];
     bf16x8 pf[N][2];
     const float scale = p.scale_log2;
-    auto read_k = [&](const unsigned char* st, int i) { return *reinterpret_cast<const bf16x8*>(st + kat[i]); };
-    auto read_v = [&](const unsigned char* st, int i) {
+    // (What differs between the pieces of a lane lies in bits of the address that its row does not touch: one register and an exclusive or.)
+    auto read_k = [&](unsigned st, int i) { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)((st + kat) ^ (i * 32)); };
+    auto read_v = [&](unsigned st, int i) {
         union {
             short4v s[2];
             bf16x8 v;
         } f;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(st + (i / X::DB) * 16 * ROW + vat[i % X::DB][h]));
+            f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) short4v*)(uintptr_t)(((st + vat) ^ (i % X::DB * 64 + h * 32)) + HALF + (i / X::DB * 16 + h * 8) * ROW));
         return f.v;
     };
     auto weigh = [&](int i) {  // scores of group i: weights, their sums
@@ -641,7 +642,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         for (int t = 0; t < N; ++t) mfma_output(o[t][i % X::DB], v, pf[t][i / X::DB]);
     };
     // 32 keys are weighed and multiplied with V (at vst) while the next 32, at kst, key kb on, are multiplied with Q
-    auto step = [&](const unsigned char* vst, const unsigned char* kst, int kb, int have) {
+    auto step = [&](unsigned vst, unsigned kst, int kb, int have) {
         bf16x8 f[QG + VG];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) f[i] = read_k(kst, i);
@@ -669,7 +670,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
 #pragma unroll
     for (int t = 0; t < N; ++t) m_use[t] = 0.f, mx[t] = -INFINITY;
     int have = next(lo);
-    const unsigned char* st = lds + (lo % kStages) * STAGE;
+    unsigned st = lo % kStages * STAGE;
 #pragma unroll
     for (int i = 0; i < QG; ++i) multiply_k(i, read_k(st, i));
     mfma_done();
@@ -677,18 +678,17 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
 #pragma unroll
     for (int i = 0; i < VG; ++i) take(i);
     settle();
-    for (int it = lo; it < hi; ++it) {
-        step(st, st + 32 * ROW, it * kWideTile + 32, have >> 2);
-        if (it + 1 == hi) break;
-        have = next(it + 1);
-        const unsigned char* after = lds + ((it + 1) % kStages) * STAGE;
-        step(st + 32 * ROW, after, (it + 1) * kWideTile, have);
-        st = after;
+    for (int j = 2 * lo + 1; j < 2 * hi; ++j) {  // (one copy of the step: two, for the two halves of a tile, kept their state in different registers)
+        const unsigned before = st;
+        have >>= 2;
+        if ((j & 1) == 0) have = next(j >> 1);
+        st = (j >> 1) % kStages * STAGE + (j & 1) * 32 * ROW;
+        step(before, st, j * 32, have);
     }
 #pragma unroll
     for (int i = 0; i < QG; ++i) weigh(i);
 #pragma unroll
-    for (int i = 0; i < VG; ++i) multiply_v(i, read_v(st + 32 * ROW, i));
+    for (int i = 0; i < VG; ++i) multiply_v(i, read_v(st, i));
     mfma_done();
 }
 
@@ -717,12 +717,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
             if (i == wave) ahead = e;
         }
     };
-    unsigned src[X::NLD];
-#pragma unroll
-    for (int i = 0; i < X::NLD; ++i) {
-        const int r = i * X::RPI + v_row;
-        src[i] = (unsigned)r * (unsigned)p.page_t + (v_slot ^ spread<D>(r)) * 16;
-    }
+    const unsigned row_off = (unsigned)v_row * (unsigned)p.page_t;
     const unsigned to = lds_address(lds) + wave * kPgGroup * ROW;
     int have_1 = 0, have_2 = 0;  // of the next two tiles
     auto fetch = [&](int it) {
@@ -734,8 +729,9 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         const unsigned stage = to + it % kStages * STAGE;
 #pragma unroll
         for (int i = 0; i < X::NLD; ++i) {
-            load_to_lds(kr, src[i], stage + i * 1024);
-            load_to_lds(vr, src[i], stage + HALF + i * 1024);
+            const unsigned off = row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (v_slot ^ spread<D>(i * X::RPI + v_row)) * 16;
+            load_to_lds(kr, off, stage + i * 1024);
+            load_to_lds(vr, off, stage + HALF + i * 1024);
         }
         return __builtin_amdgcn_readlane(ahead_have, it - ahead_from);
     };
@@ -763,15 +759,9 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     }
     // where the lane finds its pieces in a stage
     const int blk = lane >> 4, i16 = lane & 15;
-    int kat[X::KS], vat[X::DB][2];
-#pragma unroll
-    for (int s = 0; s < X::KS; ++s) kat[s] = ln * ROW + ((2 * s + hh) ^ spread<D>(ln & 15)) * 16;
+    const unsigned lds0 = lds_address(lds), kat = lds0 + ln * ROW + (hh ^ spread<D>(ln & 15)) * 16;
     const int vr = (blk >> 1) * 4 + (i16 >> 2);
-#pragma unroll
-    for (int db = 0; db < X::DB; ++db)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            vat[db][h] = HALF + (vr + h * 8) * ROW + ((db * 4 + (blk & 1) * 2 + (i16 >> 1 & 1)) ^ spread<D>(vr + h * 8)) * 16 + (i16 & 1) * 8;
+    const unsigned vat = lds0 + vr * ROW + (((blk & 1) * 2 + (i16 >> 1 & 1)) ^ spread<D>(vr)) * 16 + (i16 & 1) * 8;
     f32x16 oacc[TW][X::DB];
     float m_run[TW], l_run[TW];
 #pragma unroll
@@ -785,9 +775,9 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     }
     const int row_tiles = __builtin_amdgcn_readfirstlane((g.nrows + 31) / 32 - wave);  // from this wavefront's first on
     if (row_tiles > kPgWaves) {
-        wide_rows<D, 2>(p, g.lo, g.hi, lds, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
+        wide_rows<D, 2>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
     } else if (row_tiles > 0) {
-        wide_rows<D, 1>(p, g.lo, g.hi, lds, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
+        wide_rows<D, 1>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
     } else {
         for (int j = g.lo; j < g.hi; ++j) next(j);
     }
@@ -829,7 +819,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 template <int D, int NARROW_TILES, bool WIDE>
 __global__ __launch_bounds__(kPgThreads, !WIDE && NARROW_TILES == 1 ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
     constexpr int WIDE_LDS = kStages * kWideTile * 2 * D * 2;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[WIDE && WIDE_LDS > Tile<D>::LDS ? WIDE_LDS : Tile<D>::LDS];
+    __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > Tile<D>::LDS ? WIDE_LDS : Tile<D>::LDS];
     __shared__ float sh_m[kPgWaves][32], sh_l[kPgWaves][32];
     __shared__ int sh;
     const int lane = threadIdx.x & (kWave - 1);
