@@ -539,7 +539,8 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
     constexpr int QG = X::KS, VG = 2 * X::DB;   // groups of products with 32 keys of K and of V, N products each
-    constexpr int QE = 16 / QG, VE = 16 / VG;   // scores of a row tile that a group takes care of
+    constexpr int VE = 16 / VG;                 // scores of a row tile that a group with V takes from the next 32 keys
+    constexpr int EARLY = 6;                    // of the 8 pairs of weights of a row tile: beside the products with K; the others beside the first with V
     constexpr int AHEAD = 3;                    // groups between a read from LDS and its use
     constexpr int WAIT = 3 - N;                 // groups with V, N products each, in front of the first look at the scores
     float s[N][16], m_use[N], mx[N];
@@ -559,39 +560,27 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
                 (__attribute__((address_space(3))) short4v*)(uintptr_t)(((st + vat) ^ (i % X::DB * 64 + h * 32)) + HALF + (i / X::DB * 16 + h * 8) * ROW));
         return f.v;
     };
-    auto weigh = [&](int i) {  // scores of group i: weights, their sums
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-#pragma unroll
-            for (int e = 0; e < QE; ++e) {
-                const int x = i * QE + e;
-                s[t][x] = __builtin_amdgcn_exp2f(s[t][x] - m_use[t]);
-                l[t] += s[t][x];
-            }
-            // (pinned where they are computed: the compiler would move them down to the products that use them, behind the mask's branch)
-            asm volatile("" : "+v"(l[t]));
-#pragma unroll
-            for (int e = 0; e < QE; e += 2) {
-                const int x = i * QE + e;
-                u32x4 all = __builtin_bit_cast(u32x4, pf[t][x >> 3]);
-                // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
-                const f32x2 pair = {s[t][x], s[t][x + 1]};
-                unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, bf16x2));
-                asm volatile("" : "+v"(u));
-                all[(x & 7) >> 1] = u;
-                pf[t][x >> 3] = __builtin_bit_cast(bf16x8, all);
-            }
-        }
+    auto weigh = [&](int t, int x) {  // scores x and x + 1 of row tile t: weights, their sum
+        s[t][x] = __builtin_amdgcn_exp2f(s[t][x] - m_use[t]);
+        s[t][x + 1] = __builtin_amdgcn_exp2f(s[t][x + 1] - m_use[t]);
+        l[t] += s[t][x];
+        l[t] += s[t][x + 1];
+        // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
+        const f32x2 pair = {s[t][x], s[t][x + 1]};
+        unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, bf16x2));
+        // (pinned where they are computed: the compiler would move them down to the products that use them, behind the mask's branch)
+        asm volatile("" : "+v"(l[t]), "+v"(u));
+        u32x4 all = __builtin_bit_cast(u32x4, pf[t][x >> 3]);
+        all[(x & 7) >> 1] = u;
+        pf[t][x >> 3] = __builtin_bit_cast(bf16x8, all);
     };
-    auto take = [&](int i) {  // scores of group i of the next 32 keys: scaled, maximum
+    auto take = [&](int t, int i) {  // scores of group i of the next 32 keys: scaled, maximum
 #pragma unroll
-        for (int t = 0; t < N; ++t)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const int x = i * VE + e;
-                s[t][x] = n[t][x] * scale;
-                mx[t] = fmaxf(mx[t], s[t][x]);
-            }
+        for (int e = 0; e < VE; ++e) {
+            const int x = i * VE + e;
+            s[t][x] = n[t][x] * scale;
+            mx[t] = fmaxf(mx[t], s[t][x]);
+        }
     };
     auto mask = [&](int kb, int have) {
         if ((have & 3) == 3 && kb + 32 <= first_lim) return;
@@ -630,17 +619,11 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
 #pragma unroll
         for (int t = 0; t < N; ++t) mx[t] = -INFINITY;
     };
-    auto multiply_k = [&](int i, const bf16x8& k) {
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-            if (i == 0) mfma_first(n[t], k, qf[t][i]);
-            else mfma_scores(n[t], k, qf[t][i]);
-        }
+    auto multiply_k = [&](int t, int i, const bf16x8& k) {
+        if (i == 0) mfma_first(n[t], k, qf[t][i]);
+        else mfma_scores(n[t], k, qf[t][i]);
     };
-    auto multiply_v = [&](int i, const bf16x8& v) {
-#pragma unroll
-        for (int t = 0; t < N; ++t) mfma_output(o[t][i % X::DB], v, pf[t][i / X::DB]);
-    };
+    auto multiply_v = [&](int t, int i, const bf16x8& v) { mfma_output(o[t][i % X::DB], v, pf[t][i / X::DB]); };
     // 32 keys are weighed and multiplied with V (at vst) while the next 32, at kst, key kb on, are multiplied with Q
     auto step = [&](unsigned vst, unsigned kst, int kb, int have) {
         bf16x8 f[QG + VG];
@@ -650,21 +633,34 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         for (int i = 0; i < QG; ++i) {
             __builtin_amdgcn_sched_barrier(0);
             f[i + AHEAD] = i + AHEAD < QG ? read_k(kst, i + AHEAD) : read_v(vst, i + AHEAD - QG);
-            multiply_k(i, f[i]);
-            weigh(i);
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                multiply_k(t, i, f[i]);
+#pragma unroll
+                for (int x = i * EARLY / QG; x < (i + 1) * EARLY / QG; ++x) weigh(t, 2 * x);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        __builtin_amdgcn_sched_barrier(0);
         mask(kb, have);
 #pragma unroll
         for (int i = 0; i < VG; ++i) {
             __builtin_amdgcn_sched_barrier(0);
             if (i + AHEAD < VG) f[QG + i + AHEAD] = read_v(vst, i + AHEAD);
-            multiply_v(i, f[QG + i]);
-            if (i >= WAIT) take(i - WAIT);
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                multiply_v(t, i, f[QG + i]);
+                if (i < X::DB) {
+#pragma unroll
+                    for (int x = EARLY + i * (8 - EARLY) / X::DB; x < EARLY + (i + 1) * (8 - EARLY) / X::DB; ++x) weigh(t, 2 * x);
+                }
+                if (i >= WAIT) take(t, i - WAIT);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
 #pragma unroll
-        for (int i = VG - WAIT; i < VG; ++i) take(i);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = VG - WAIT; i < VG; ++i)
+#pragma unroll
+            for (int t = 0; t < N; ++t) take(t, i);
         settle();
     };
 #pragma unroll
@@ -672,11 +668,17 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     int have = next(lo);
     unsigned st = lo % kStages * STAGE;
 #pragma unroll
-    for (int i = 0; i < QG; ++i) multiply_k(i, read_k(st, i));
+    for (int i = 0; i < QG; ++i) {
+        const bf16x8 k = read_k(st, i);
+#pragma unroll
+        for (int t = 0; t < N; ++t) multiply_k(t, i, k);
+    }
     mfma_done();
     mask(lo * kWideTile, have);
 #pragma unroll
-    for (int i = 0; i < VG; ++i) take(i);
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int i = 0; i < VG; ++i) take(t, i);
     settle();
     for (int j = 2 * lo + 1; j < 2 * hi; ++j) {  // (one copy of the step: two, for the two halves of a tile, kept their state in different registers)
         const unsigned before = st;
@@ -686,9 +688,15 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         step(before, st, j * 32, have);
     }
 #pragma unroll
-    for (int i = 0; i < QG; ++i) weigh(i);
+    for (int t = 0; t < N; ++t)
 #pragma unroll
-    for (int i = 0; i < VG; ++i) multiply_v(i, read_v(st, i));
+        for (int x = 0; x < 16; x += 2) weigh(t, x);
+#pragma unroll
+    for (int i = 0; i < VG; ++i) {
+        const bf16x8 v = read_v(st, i);
+#pragma unroll
+        for (int t = 0; t < N; ++t) multiply_v(t, i, v);
+    }
     mfma_done();
 }
 
