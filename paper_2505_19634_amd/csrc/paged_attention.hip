@@ -528,25 +528,28 @@ __device__ __forceinline__ void mfma_output(f32x16& d, const bf16x8& a, const bf
 }
 __device__ __forceinline__ void mfma_done() { asm volatile("s_nop 15\n\ts_nop 15"); }
 
-// The loop over a wide item's tiles for a wavefront with N row tiles.  next(j) brings tile j in: it waits for its loads and for the other wavefronts,
-// and requests one more.  While the matrix cores multiply K of tile j + 1 with Q, the vector units turn the scores of tile j into weights; then V of
-// tile j is multiplied while the scores of tile j + 1 are scaled and their maximum is taken.  A wavefront has its SIMD to itself and issues in
-// order, so the two streams are written down interleaved, a pair of products and its share of the vector work at a time, and the
-// scheduling barriers keep them so.
-template <int D, int N, typename Next>
+// The loop over a wide item's tiles for a wavefront with N row tiles.  arrive(): the next tile is in LDS for everybody; request(j, v, i): load i of the
+// wavefront's part of tile j's K or V.  In a step 32 keys are weighed and multiplied with V while the next 32 are multiplied with Q and their maximum
+// is found.  A wavefront has its SIMD to itself and issues in order: a product takes its 32 cycles beside whatever comes behind it, but a
+// vector instruction that needs the one before it waits 8 cycles (independent ones take 4 to 5, an exponential 9).  So the step is
+// written down as slots of one product each, and a pair of weights goes through three of them -- scaled, exponential, rounded and summed -- so
+// that nothing in a slot depends on anything else in it; scheduling barriers keep the slots apart.  (With a pair's whole chain in one slot a step of 2 row
+// tiles took 2300 cycles, the products alone take 1024.)
+template <int D, int N, typename Arrive, typename Request>
 __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[2][Tile<D>::KS], const int (&lim)[2],
-                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[2][Tile<D>::DB], float (&m)[2], float (&l)[2], Next next) {
+                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[2][Tile<D>::DB], float (&m)[2], float (&l)[2], Arrive arrive, Request request) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
     constexpr int QG = X::KS, VG = 2 * X::DB;   // groups of products with 32 keys of K and of V, N products each
-    constexpr int VE = 16 / VG;                 // scores of a row tile that a group with V takes from the next 32 keys
-    constexpr int EARLY = 6;                    // of the 8 pairs of weights of a row tile: beside the products with K; the others beside the first with V
+    constexpr int QS = QG * N, VS = VG * N;     // slots
     constexpr int AHEAD = 3;                    // groups between a read from LDS and its use
-    constexpr int WAIT = 3 - N;                 // groups with V, N products each, in front of the first look at the scores
-    float s[N][16], m_use[N], mx[N];
-    f32x16 n[N];
+    constexpr int PAIRS = 8 * N;                // pairs of weights: the first half goes into the first half of the products with V
+    constexpr int SPAN = (QG + X::DB) * N - (D == 64 ? 3 : 2);  // slots over which they begin: done two slots before their product
+    constexpr int LOOK = QS + 2, LOOKS = VS - 3;  // slots that look at the next scores: two products behind the last one that makes them, up to the last but one
+    float negm[N], mx[N], l2[N];  // l2: the sums of every second weight
+    f32x16 sa[N], sb[N];  // scores as products leave them, in turns: of the keys that are weighed, of the next ones
     bf16x8 pf[N][2];
-    const float scale = p.scale_log2;
+    const float scale = p.scale_log2, rescale = kRescale / scale;
     // (What differs between the pieces of a lane lies in bits of the address that its row does not touch: one register and an exclusive or.)
     auto read_k = [&](unsigned st, int i) { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)((st + kat) ^ (i * 32)); };
     auto read_v = [&](unsigned st, int i) {
@@ -560,29 +563,53 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
                 (__attribute__((address_space(3))) short4v*)(uintptr_t)(((st + vat) ^ (i % X::DB * 64 + h * 32)) + HALF + (i / X::DB * 16 + h * 8) * ROW));
         return f.v;
     };
-    auto weigh = [&](int t, int x) {  // scores x and x + 1 of row tile t: weights, their sum
-        s[t][x] = __builtin_amdgcn_exp2f(s[t][x] - m_use[t]);
-        s[t][x + 1] = __builtin_amdgcn_exp2f(s[t][x + 1] - m_use[t]);
-        l[t] += s[t][x];
-        l[t] += s[t][x + 1];
+    // (Every result is pinned where it is computed: the compiler would move it down to its use, behind the mask's branch.)
+    auto scale_pair = [&](f32x16 (&c)[N], int q) {
+        const int t = q % N, x = q / N * 2;
+        float u = __builtin_fmaf(c[t][x], scale, negm[t]), v = __builtin_fmaf(c[t][x + 1], scale, negm[t]);
+        asm volatile("" : "+v"(u), "+v"(v));
+        c[t][x] = u;
+        c[t][x + 1] = v;
+    };
+    auto weigh_pair = [&](f32x16 (&c)[N], int q) {
+        const int t = q % N, x = q / N * 2;
+        float u = __builtin_amdgcn_exp2f(c[t][x]), v = __builtin_amdgcn_exp2f(c[t][x + 1]);
+        asm volatile("" : "+v"(u), "+v"(v));
+        c[t][x] = u;
+        c[t][x + 1] = v;
+    };
+    auto sum_pair = [&](f32x16 (&c)[N], int q) {
+        const int t = q % N, x = q / N * 2;
         // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
-        const f32x2 pair = {s[t][x], s[t][x + 1]};
+        const f32x2 pair = {c[t][x], c[t][x + 1]};
         unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, bf16x2));
-        // (pinned where they are computed: the compiler would move them down to the products that use them, behind the mask's branch)
-        asm volatile("" : "+v"(l[t]), "+v"(u));
+        l[t] += c[t][x];
+        l2[t] += c[t][x + 1];
+        asm volatile("" : "+v"(l[t]), "+v"(l2[t]), "+v"(u));
         u32x4 all = __builtin_bit_cast(u32x4, pf[t][x >> 3]);
         all[(x & 7) >> 1] = u;
         pf[t][x >> 3] = __builtin_bit_cast(bf16x8, all);
     };
-    auto take = [&](int t, int i) {  // scores of group i of the next 32 keys: scaled, maximum
+    auto look = [&](const f32x16 (&n)[N], int r) {  // a pair of the next scores
+        const int t = r % N, x = r / N * 2;
+        mx[t] = fmaxf(fmaxf(mx[t], n[t][x]), n[t][x + 1]);
+        asm volatile("" : "+v"(mx[t]));
+    };
+    // what goes beside the product of slot i
+    auto beside = [&](f32x16 (&c)[N], const f32x16 (&n)[N], int i) {
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            const int x = i * VE + e;
-            s[t][x] = n[t][x] * scale;
-            mx[t] = fmaxf(mx[t], s[t][x]);
+        for (int q = 0; q < PAIRS; ++q) {
+            if (q * SPAN / PAIRS + 2 == i) sum_pair(c, q);
+            if (q * SPAN / PAIRS + 1 == i) weigh_pair(c, q);
+            if (q * SPAN / PAIRS == i) scale_pair(c, q);
+        }
+        if (i >= LOOK) {
+#pragma unroll
+            for (int r = 0; r < PAIRS; ++r)
+                if (LOOK + r * LOOKS / PAIRS == i) look(n, r);
         }
     };
-    auto mask = [&](int kb, int have) {
+    auto mask = [&](f32x16 (&n)[N], int kb, int have) {
         if ((have & 3) == 3 && kb + 32 <= first_lim) return;
         mfma_done();
         const int hh = (threadIdx.x & 32) >> 5;
@@ -593,23 +620,24 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
             for (int x = 0; x < 16; ++x) n[t][x] = (x >> 2) * 8 + (x & 3) < vis && (have >> (x >> 3) & 1) ? n[t][x] : -INFINITY;
         }
     };
-    auto settle = [&] {  // the running maximum of the scores in s; o and l follow where it has risen much
-        bool rise[N], any = false;
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-            mx[t] = max_halves(mx[t]);
-            rise[t] = mx[t] > m[t] + kRescale;
-            any = any || rise[t];
-        }
+    bool rise[N];
+    auto find_rise = [&](int t) {
+        mx[t] = max_halves(mx[t]);
+        rise[t] = mx[t] > m[t] + rescale;
+    };
+    auto settle = [&] {  // o and l follow where the maximum has risen much
+        bool any = rise[0];
+        if (N > 1) any = any || rise[N - 1];
         if (__builtin_amdgcn_ballot_w64(any) != 0) {
             mfma_done();
 #pragma unroll
             for (int t = 0; t < N; ++t) {
                 const float m_new = rise[t] ? mx[t] : m[t], base = m_new == -INFINITY ? 0.f : m_new;
-                const float alpha = __builtin_amdgcn_exp2f(m[t] - base);
+                const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * scale);
                 m[t] = m_new;
-                m_use[t] = base;
+                negm[t] = -base * scale;
                 l[t] *= alpha;
+                l2[t] *= alpha;
 #pragma unroll
                 for (int db = 0; db < X::DB; ++db)
 #pragma unroll
@@ -619,85 +647,100 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
 #pragma unroll
         for (int t = 0; t < N; ++t) mx[t] = -INFINITY;
     };
-    auto multiply_k = [&](int t, int i, const bf16x8& k) {
+    auto multiply_k = [&](f32x16 (&n)[N], int t, int i, const bf16x8& k) {
         if (i == 0) mfma_first(n[t], k, qf[t][i]);
         else mfma_scores(n[t], k, qf[t][i]);
     };
     auto multiply_v = [&](int t, int i, const bf16x8& v) { mfma_output(o[t][i % X::DB], v, pf[t][i / X::DB]); };
-    // 32 keys are weighed and multiplied with V (at vst) while the next 32, at kst, key kb on, are multiplied with Q
-    auto step = [&](unsigned vst, unsigned kst, int kb, int have) {
+    bf16x8 k0[AHEAD];  // the first pieces of K of the step ahead
+    int have;
+    unsigned st = lo % kStages * STAGE;
+    // Step j: the scores in c, of the keys at st, are weighed and multiplied with V, those of the j-th 32 keys of all go into n.
+    auto step = [&](f32x16 (&c)[N], f32x16 (&n)[N], int j) {
+        const unsigned before = st;
+        st = (j >> 1) % kStages * STAGE + (j & 1) * 32 * ROW;
+        have >>= 2;
         bf16x8 f[QG + VG];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) f[i] = read_k(kst, i);
+        for (int i = 0; i < AHEAD; ++i) f[i] = k0[i];
 #pragma unroll
         for (int i = 0; i < QG; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            f[i + AHEAD] = i + AHEAD < QG ? read_k(kst, i + AHEAD) : read_v(vst, i + AHEAD - QG);
+            f[i + AHEAD] = i + AHEAD < QG ? read_k(st, i + AHEAD) : read_v(before, i + AHEAD - QG);
 #pragma unroll
             for (int t = 0; t < N; ++t) {
-                multiply_k(t, i, f[i]);
-#pragma unroll
-                for (int x = i * EARLY / QG; x < (i + 1) * EARLY / QG; ++x) weigh(t, 2 * x);
+                multiply_k(n, t, i, f[i]);
+                beside(c, n, i * N + t);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (i % (2 * QG / X::NLD) == QG / X::NLD) request((j >> 1) + 2, j & 1, i * X::NLD / (2 * QG));
         }
-        mask(kb, have);
+        if (D == 64) asm volatile("s_nop 1");  // (the first half's last weights were rounded in the slot before)
+        mask(n, j * 32, have);
+        // the tile of the next step's K, so that its first pieces are read beside the products with V
+        if ((j & 1) != 0 && j + 1 < 2 * hi) have = arrive(false) << 2;
+        const unsigned after = ((j + 1) >> 1) % kStages * STAGE + ((j + 1) & 1) * 32 * ROW;
 #pragma unroll
         for (int i = 0; i < VG; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            if (i + AHEAD < VG) f[QG + i + AHEAD] = read_v(vst, i + AHEAD);
+            if (i + AHEAD < VG) f[QG + i + AHEAD] = read_v(before, i + AHEAD);
+            else k0[i + AHEAD - VG] = read_k(after, i + AHEAD - VG);
 #pragma unroll
             for (int t = 0; t < N; ++t) {
                 multiply_v(t, i, f[QG + i]);
-                if (i < X::DB) {
-#pragma unroll
-                    for (int x = EARLY + i * (8 - EARLY) / X::DB; x < EARLY + (i + 1) * (8 - EARLY) / X::DB; ++x) weigh(t, 2 * x);
-                }
-                if (i >= WAIT) take(t, i - WAIT);
+                beside(c, n, QS + i * N + t);
+                if (i == VG - 1) find_rise(t);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (i % (2 * VG / X::NLD) == VG / X::NLD) request((j >> 1) + 2, j & 1, X::NLD / 2 + i * X::NLD / (2 * VG));
         }
-#pragma unroll
-        for (int i = VG - WAIT; i < VG; ++i)
-#pragma unroll
-            for (int t = 0; t < N; ++t) take(t, i);
         settle();
     };
+    // the last scores: nothing is left to multiply with Q
+    auto finish = [&](f32x16 (&c)[N]) {
 #pragma unroll
-    for (int t = 0; t < N; ++t) m_use[t] = 0.f, mx[t] = -INFINITY;
-    int have = next(lo);
-    unsigned st = lo % kStages * STAGE;
+        for (int q = 0; q < PAIRS; ++q) scale_pair(c, q);
+#pragma unroll
+        for (int q = 0; q < PAIRS; ++q) weigh_pair(c, q);
+#pragma unroll
+        for (int q = 0; q < PAIRS; ++q) sum_pair(c, q);
+        asm volatile("s_nop 1");
+#pragma unroll
+        for (int i = 0; i < VG; ++i) {
+            const bf16x8 v = read_v(st, i);
+#pragma unroll
+            for (int t = 0; t < N; ++t) multiply_v(t, i, v);
+        }
+        mfma_done();
+    };
+#pragma unroll
+    for (int t = 0; t < N; ++t) negm[t] = 0.f, mx[t] = -INFINITY, l2[t] = 0.f;
+    have = arrive(true);
+#pragma unroll
+    for (int i = 0; i < X::NLD; ++i) request(lo + 2, 0, i);
 #pragma unroll
     for (int i = 0; i < QG; ++i) {
         const bf16x8 k = read_k(st, i);
 #pragma unroll
-        for (int t = 0; t < N; ++t) multiply_k(t, i, k);
+        for (int t = 0; t < N; ++t) multiply_k(sa, t, i, k);
     }
     mfma_done();
-    mask(lo * kWideTile, have);
+    mask(sa, lo * kWideTile, have);
 #pragma unroll
-    for (int t = 0; t < N; ++t)
+    for (int r = 0; r < PAIRS; ++r) look(sa, r);
 #pragma unroll
-        for (int i = 0; i < VG; ++i) take(t, i);
+    for (int t = 0; t < N; ++t) find_rise(t);
     settle();
-    for (int j = 2 * lo + 1; j < 2 * hi; ++j) {  // (one copy of the step: two, for the two halves of a tile, kept their state in different registers)
-        const unsigned before = st;
-        have >>= 2;
-        if ((j & 1) == 0) have = next(j >> 1);
-        st = (j >> 1) % kStages * STAGE + (j & 1) * 32 * ROW;
-        step(before, st, j * 32, have);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) k0[i] = read_k(st + 32 * ROW, i);
+    for (int it = lo; it + 1 < hi; ++it) {
+        step(sa, sb, 2 * it + 1);
+        step(sb, sa, 2 * it + 2);
     }
+    step(sa, sb, 2 * hi - 1);
+    finish(sb);
 #pragma unroll
-    for (int t = 0; t < N; ++t)
-#pragma unroll
-        for (int x = 0; x < 16; x += 2) weigh(t, x);
-#pragma unroll
-    for (int i = 0; i < VG; ++i) {
-        const bf16x8 v = read_v(st, i);
-#pragma unroll
-        for (int t = 0; t < N; ++t) multiply_v(t, i, v);
-    }
-    mfma_done();
+    for (int t = 0; t < N; ++t) l[t] += l2[t];
 }
 
 // The workgroup loads a tile together, 16 keys a wavefront; wavefront w takes the row tiles w and w + 4 of the item.
@@ -713,7 +756,10 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     const int keys = max(0, before + quot(g.row0 + g.nrows - 1, p.d_g) + 1);
     const int first_lim = before + quot(min(g.row0 + wave * 32, g.row0 + g.nrows - 1), p.d_g) + 1;  // what all rows of the wavefront see
     const int v_row = lane / X::LPR, v_slot = lane % X::LPR;
-    int ahead = 0, ahead_have = 0, ahead_from = 0;  // the wavefront's own entry of a tile; which of its four groups have one
+    // Lane i knows of tile ahead_from + i: where the wavefront's 16 keys lie, how many bytes of them there are (none without a page, and behind
+    // the last key), and which of the tile's four groups have a page.
+    unsigned ahead_lo = 0, ahead_hi = 0, ahead_bytes = 0;
+    int ahead_have = 0, ahead_from = 0;
     auto look_ahead = [&](int it) {
         ahead_from = it;
         ahead_have = 0;
@@ -722,37 +768,52 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         for (int i = 0; i < kWideTile / kPgGroup; ++i) {
             const int e = page_entry(p, row, kb + i * kPgGroup);
             if ((unsigned)e < (unsigned)p.pages) ahead_have |= 1 << i;
-            if (i == wave) ahead = e;
+            if (i == wave) {
+                const long long at = group_at(p, e, kb + i * kPgGroup, g.kvh);
+                ahead_lo = (unsigned)at;
+                ahead_hi = (unsigned)(at >> 32);
+                ahead_bytes = group_bytes(p, e, kb + i * kPgGroup, keys, D * 2);
+            }
         }
     };
     const unsigned row_off = (unsigned)v_row * (unsigned)p.page_t;
+    unsigned piece = (v_slot ^ spread<D>(v_row)) * 16;  // of the first load; the others' differ in the bits that spread() takes from the row's upper part
     const unsigned to = lds_address(lds) + wave * kPgGroup * ROW;
-    int have_1 = 0, have_2 = 0;  // of the next two tiles
-    auto fetch = [&](int it) {
-        if (it - ahead_from >= kWave) look_ahead(it);
-        const int e = __builtin_amdgcn_readlane(ahead, it - ahead_from), key = it * kWideTile + wave * kPgGroup;
-        const unsigned bytes = group_bytes(p, e, key, keys, D * 2);
-        const long long at = group_at(p, e, key, g.kvh);
-        const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes), vr = buffer((const unsigned char*)p.V + at, bytes);
-        const unsigned stage = to + it % kStages * STAGE;
-#pragma unroll
-        for (int i = 0; i < X::NLD; ++i) {
-            const unsigned off = row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (v_slot ^ spread<D>(i * X::RPI + v_row)) * 16;
-            load_to_lds(kr, off, stage + i * 1024);
-            load_to_lds(vr, off, stage + HALF + i * 1024);
+    int have_0 = 0, have_1 = 0;  // of the tile that arrives next and of the one behind it
+    const unsigned long long k_to_v = (unsigned long long)p.V - (unsigned long long)p.K;
+    unsigned long long at = 0;
+    unsigned bytes = 0, stage = 0;
+    // Tiles behind the last one are requested too, with no bytes in range: every wait counts the same loads.
+    auto request = [&](int it, int v, int i) {
+        if (i == 0 && v == 0) {
+            if (it - ahead_from >= kWave) look_ahead(it);
+            const int x = it - ahead_from;
+            at = (unsigned long long)(unsigned)__builtin_amdgcn_readlane(ahead_hi, x) << 32 | (unsigned)__builtin_amdgcn_readlane(ahead_lo, x);
+            bytes = __builtin_amdgcn_readlane(ahead_bytes, x);
+            have_1 = __builtin_amdgcn_readlane(ahead_have, x);
+            stage = to + it % kStages * STAGE;
         }
-        return __builtin_amdgcn_readlane(ahead_have, it - ahead_from);
+        unsigned first = piece;
+        asm volatile("" : "+v"(first));  // (formed where it is used: four offsets are three registers more)
+        load_to_lds(buffer((const unsigned char*)p.K + (long long)(at + (k_to_v & (unsigned long long)-(long long)v)), bytes), row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (first ^ spread<D>(i * X::RPI) * 16),
+                    stage + v * HALF + i * 1024);
     };
     look_ahead(g.lo);
-    have_1 = fetch(g.lo);
-    if (g.lo + 1 < g.hi) have_2 = fetch(g.lo + 1);
-    // Tile j is in LDS for everybody; everybody has left tile j - 2 behind, whose stage the next request takes.
-    auto next = [&](int j) {
-        if (j + 1 < g.hi) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * X::NLD) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const int have = have_1;
-        have_1 = have_2;
-        if (j + 2 < g.hi) have_2 = fetch(j + 2);
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int i = 0; i < X::NLD; ++i) request(g.lo + tile, v, i);
+        if (tile == 0) have_0 = have_1;
+    }
+    // The next tile is in LDS for everybody; everybody has left the tile before the last behind, whose stage the next requests take.  Loads behind
+    // the tile's that are on their way: K and V of the next one at first, then K and half of V of the next one.
+    auto arrive_tile = [&](bool first) {
+        if (first) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * X::NLD) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(X::NLD + X::NLD / 2) : "memory");
+        const int have = have_0;
+        have_0 = have_1;
         return have;
     };
     bf16x8 qf[TW][X::KS];
@@ -783,12 +844,24 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     }
     const int row_tiles = __builtin_amdgcn_readfirstlane((g.nrows + 31) / 32 - wave);  // from this wavefront's first on
     if (row_tiles > kPgWaves) {
-        wide_rows<D, 2>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
+        wide_rows<D, 2>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
     } else if (row_tiles > 0) {
-        wide_rows<D, 1>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, next);
-    } else {
-        for (int j = g.lo; j < g.hi; ++j) next(j);
+        wide_rows<D, 1>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
+    } else {  // no rows: the loads and the meetings alone, in the same order
+        arrive_tile(true);
+#pragma unroll
+        for (int i = 0; i < X::NLD; ++i) request(g.lo + 2, 0, i);
+        for (int j = g.lo; j + 1 < g.hi; ++j) {
+#pragma unroll
+            for (int i = 0; i < X::NLD / 2; ++i) request(j + 2, 1, i);
+            arrive_tile(false);
+#pragma unroll
+            for (int i = X::NLD / 2; i < X::NLD; ++i) request(j + 2, 1, i);
+#pragma unroll
+            for (int i = 0; i < X::NLD; ++i) request(j + 3, 0, i);
+        }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
@@ -803,7 +876,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
                 for (int q = 0; q < 4; ++q)
                     part_store4(rs, p.off_o + (at * D + db * 32 + q * 8 + hh * 4) * 4u,
                                 make_float4(oacc[t][db][q * 4], oacc[t][db][q * 4 + 1], oacc[t][db][q * 4 + 2], oacc[t][db][q * 4 + 3]));
-            if (hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run[t], l));
+            if (hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run[t] * p.scale_log2, l));
             continue;
         }
         const int i = quot(g.row0 + r, p.d_g), h = g.kvh * p.G + g.row0 + r - i * p.G;
@@ -818,7 +891,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
                 for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oacc[t][db][q * 4 + e] * inv);
                 *reinterpret_cast<bf16x4*>(op + (db * 32 + q * 8 + hh * 4) * 2) = v;
             }
-        if (p.lse && hh == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (m_run[t] + log2f(l)) * 0.69314718055994530942f;
+        if (p.lse && hh == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (m_run[t] * p.scale_log2 + log2f(l)) * 0.69314718055994530942f;
     }
     if (g.parts > 1) arrive<D>(p, g, rs, w, sh);
     __syncthreads();
