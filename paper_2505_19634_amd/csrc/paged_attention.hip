@@ -186,10 +186,10 @@ __device__ __forceinline__ void store_out(const PagedParams& p, const Segment& g
 __device__ __forceinline__ int part_slot(int w, int w0) { return 2 * w + (w == w0 ? 1 : 0); }
 
 // Merges partials [from, from + count) of the segment's item -- every STEP-th of them -- in their order: into the output, or in place of the first.
-template <int D>
+template <int D, int WAVES>
 __device__ __forceinline__ void merge_parts(const PagedParams& p, const Segment& g, __amdgpu_buffer_rsrc_t rs, int from, int count, int step, bool last) {
     constexpr int F4 = D / 4, CH = 8;
-    for (int e = threadIdx.x; e < g.nrows * F4; e += kPgThreads) {  // (a row's quads lie in one wavefront: what is read comes in front of what is written)
+    for (int e = threadIdx.x; e < g.nrows * F4; e += WAVES * kWave) {  // (a row's quads lie in one wavefront: what is read comes in front of what is written)
         const int r = e / F4, c4 = e - r * F4;
         float M = -INFINITY, l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -234,7 +234,7 @@ __device__ __forceinline__ void merge_parts(const PagedParams& p, const Segment&
 // The workgroup's partial of a cut item is written: it counts itself, and whoever comes last merges -- kMergeGroup neighbours first, then what
 // these have left.  Every wavefront waits for its stores before the count.  A cell starts at the call's tag, which is larger than that
 // of any earlier call, and goes back to zero: a captured launch is replayed with its tag.
-template <int D>
+template <int D, int WAVES>
 __device__ __forceinline__ void arrive(const PagedParams& p, const Segment& g, __amdgpu_buffer_rsrc_t rs, int w, int* sh) {
     auto last_of = [&](unsigned long long* cell, int count) {
         __builtin_amdgcn_s_waitcnt(0);  // the wavefront's stores are in memory
@@ -254,12 +254,12 @@ __device__ __forceinline__ void arrive(const PagedParams& p, const Segment& g, _
     const bool one_group = g.parts <= kMergeGroup;
     if (members > 1) {
         if (!last_of(p.cells + part_slot(g.w0 + first, g.w0), members)) return;
-        merge_parts<D>(p, g, rs, first, members, 1, one_group);
+        merge_parts<D, WAVES>(p, g, rs, first, members, 1, one_group);
     }
     if (one_group) return;
     const int groups = (g.parts - 1) / kMergeGroup + 1;
     if (!last_of(p.cells + 2 * p.workers + part_slot(g.w0, g.w0), groups)) return;
-    merge_parts<D>(p, g, rs, 0, groups, kMergeGroup, true);
+    merge_parts<D, WAVES>(p, g, rs, 0, groups, kMergeGroup, true);
 }
 
 // What a wavefront knows of the pages of the tiles ahead: lane i has the entries of the i-th tile from `base` on, STEP tiles apart.  One load
@@ -289,7 +289,6 @@ struct Tile {
     static constexpr int VSTRIDE = D * 2 + 64;    // (pad: conflict-free transposing reads)
     static constexpr int OSTRIDE = D + 4;         // floats per row of a parked output
     static constexpr int SLAB = kNarrowTile * (KSTRIDE + VSTRIDE);  // LDS of a wavefront (narrow)
-    static constexpr int LDS = kPgWaves * SLAB;
     static_assert(32 * OSTRIDE * 4 <= SLAB, "a parked output reuses the wavefront's slab");
 };
 
@@ -341,15 +340,15 @@ __device__ __forceinline__ bf16x8 read_v(const unsigned char* at) {
     return f.v;
 }
 
-// A narrow item's part: wavefront w takes tiles lo + w, lo + w + 4, ..., each into registers one tile ahead and through a slab of its own.
-template <int D, int TW>
+// A narrow item's part: wavefront w takes tiles lo + w, lo + w + WAVES, ..., each into registers one tile ahead and through a slab of its own.
+template <int D, int TW, int WAVES>
 __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh) {
     using X = Tile<D>;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     const int ln = lane & 31, hh = lane >> 5;
     const int32_t* row = p.table + g.b * p.table_stride;
     const int keys = min(g.L, max(0, g.L - g.n + quot(g.nrows - 1, p.d_g) + 1)), before = g.L - g.n;
-    const int n_tiles = g.lo + wave < g.hi ? (g.hi - 1 - g.lo - wave) / kPgWaves + 1 : 0;
+    const int n_tiles = g.lo + wave < g.hi ? (g.hi - 1 - g.lo - wave) / WAVES + 1 : 0;
     const int v_row = lane / X::LPR, v_chunk = lane % X::LPR;
     const int blk = lane >> 4, i16 = lane & 15;
     const int tr_off = ((blk >> 1) * 4 + (i16 >> 2)) * X::VSTRIDE + ((blk & 1) * 16 + (i16 & 3) * 4) * 2;
@@ -357,7 +356,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
     int ahead[2], ahead_from = 0;  // entries of the wavefront's tiles ahead_from .. ahead_from + 63
     auto look_ahead = [&](int it) {
         ahead_from = it;
-        const int key = (g.lo + wave + (it + lane) * kPgWaves) * kNarrowTile;
+        const int key = (g.lo + wave + (it + lane) * WAVES) * kNarrowTile;
         ahead[0] = page_entry(p, row, key);
         ahead[1] = page_entry(p, row, key + kPgGroup);
     };
@@ -365,7 +364,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
     int have_next = 0;
     auto fetch = [&](int it) {
         if (it - ahead_from >= kWave) look_ahead(it);
-        const int kb = (g.lo + wave + it * kPgWaves) * kNarrowTile;
+        const int kb = (g.lo + wave + it * WAVES) * kNarrowTile;
         have_next = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -407,7 +406,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
     }
     for (int it = 0; it < n_tiles; ++it) {
-        const int kb = (g.lo + wave + it * kPgWaves) * kNarrowTile;
+        const int kb = (g.lo + wave + it * WAVES) * kNarrowTile;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -443,7 +442,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
     }
     // the wavefronts' states of a row tile meet in LDS, in their order
     const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
-    constexpr int F4 = D / 4, QPT = 32 * F4 / kPgThreads, RSTEP = kPgThreads / F4;
+    constexpr int F4 = D / 4, QPT = 32 * F4 / (WAVES * kWave), RSTEP = (WAVES * kWave) / F4;
     const int c4 = tid % F4, row0 = tid / F4;
     float* obuf = reinterpret_cast<float*>(kslab);
 #pragma unroll
@@ -468,11 +467,11 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             if (r >= g.nrows) continue;
             float M = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int v = 0; v < kPgWaves; ++v) M = fmaxf(M, sh_m[v][rt]);
+            for (int v = 0; v < WAVES; ++v) M = fmaxf(M, sh_m[v][rt]);
             const float Mu = M == -INFINITY ? 0.f : M;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int v = 0; v < kPgWaves; ++v) {
+            for (int v = 0; v < WAVES; ++v) {
                 const float f = __builtin_amdgcn_exp2f(sh_m[v][rt] - Mu);
                 const float4 ov = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds + v * X::SLAB) + rt * X::OSTRIDE + c4 * 4);
                 sum += sh_l[v][rt] * f;
@@ -487,7 +486,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             }
         }
     }
-    if (g.parts > 1) arrive<D>(p, g, rs, w, sh);
+    if (g.parts > 1) arrive<D, WAVES>(p, g, rs, w, sh);
     __syncthreads();  // the slabs are free
 }
 
@@ -513,15 +512,21 @@ __device__ __forceinline__ unsigned lds_address(const void* at) {
 constexpr int kStages = 4;     // tiles in LDS: one whose V is read, one whose K is read, two on their way
 constexpr float kRescale = 8.f;  // a running maximum may be behind the true one by a factor of 2^8 before the state is rescaled
 
+// Loads of a wavefront for its keys of a tile, K or V.
+template <int D>
+__device__ constexpr int wide_loads() {
+    return D == 128 ? 2 : 1;
+}
+
 // The products of a wide item are written as instructions, so that every operand lies where it should: outputs and Q in accumulation registers,
 // scores where the vector units reach them.  (Left to choose, the compiler put the scores into accumulation registers too, Q into scratch memory
 // and the waits for that into the loop.)  It does not know how long these take: what reads a result on the vector units is kept behind
 // two later products, or behind mfma_done().
 __device__ __forceinline__ void mfma_first(f32x16& d, const bf16x8& a, const bf16x8& b) {
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "a"(b));
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_scores(f32x16& d, const bf16x8& a, const bf16x8& b) {
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "a"(b));
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_output(f32x16& d, const bf16x8& a, const bf16x8& b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
@@ -536,12 +541,13 @@ __device__ __forceinline__ void mfma_done() { asm volatile("s_nop 15\n\ts_nop 15
 // that nothing in a slot depends on anything else in it; scheduling barriers keep the slots apart.  (With a pair's whole chain in one slot a step of 2 row
 // tiles took 2300 cycles, the products alone take 1024.)
 template <int D, int N, typename Arrive, typename Request>
-__device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[2][Tile<D>::KS], const int (&lim)[2],
-                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[2][Tile<D>::DB], float (&m)[2], float (&l)[2], Arrive arrive, Request request) {
+__device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[N][Tile<D>::KS], const int (&lim)[N],
+                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[N][Tile<D>::DB], float (&m)[N], float (&l)[N], Arrive arrive, Request request) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
     constexpr int QG = X::KS, VG = 2 * X::DB;   // groups of products with 32 keys of K and of V, N products each
     constexpr int QS = QG * N, VS = VG * N;     // slots
+    constexpr int LOADS = wide_loads<D>(), EARLY = LOADS / 2;  // of a wavefront and operand; those beside products with K
     constexpr int AHEAD = 3;                    // groups between a read from LDS and its use
     constexpr int PAIRS = 8 * N;                // pairs of weights: the first half goes into the first half of the products with V
     constexpr int SPAN = (QG + X::DB) * N - (D == 64 ? 3 : 2);  // slots over which they begin: done two slots before their product
@@ -673,7 +679,9 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
                 beside(c, n, i * N + t);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (i % (2 * QG / X::NLD) == QG / X::NLD) request((j >> 1) + 2, j & 1, i * X::NLD / (2 * QG));
+#pragma unroll
+            for (int r = 0; r < EARLY; ++r)
+                if (i == (2 * r + 1) * QG / (2 * (EARLY > 0 ? EARLY : 1))) request((j >> 1) + 2, j & 1, r);
         }
         if (D == 64) asm volatile("s_nop 1");  // (the first half's last weights were rounded in the slot before)
         mask(n, j * 32, have);
@@ -692,7 +700,9 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
                 if (i == VG - 1) find_rise(t);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (i % (2 * VG / X::NLD) == VG / X::NLD) request((j >> 1) + 2, j & 1, X::NLD / 2 + i * X::NLD / (2 * VG));
+#pragma unroll
+            for (int r = EARLY; r < LOADS; ++r)
+                if (i == (2 * (r - EARLY) + 1) * VG / (2 * (LOADS - EARLY))) request((j >> 1) + 2, j & 1, r);
         }
         settle();
     };
@@ -717,7 +727,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     for (int t = 0; t < N; ++t) negm[t] = 0.f, mx[t] = -INFINITY, l2[t] = 0.f;
     have = arrive(true);
 #pragma unroll
-    for (int i = 0; i < X::NLD; ++i) request(lo + 2, 0, i);
+    for (int i = 0; i < LOADS; ++i) request(lo + 2, 0, i);
 #pragma unroll
     for (int i = 0; i < QG; ++i) {
         const bf16x8 k = read_k(st, i);
@@ -743,11 +753,12 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     for (int t = 0; t < N; ++t) l[t] += l2[t];
 }
 
-// The workgroup loads a tile together, 16 keys a wavefront; wavefront w takes the row tiles w and w + 4 of the item.
-template <int D>
+// The workgroup loads a tile together, 8 keys a wavefront; wavefront w takes row tile w of the item.
+template <int D, int WAVES>
 __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, int* sh) {
     using X = Tile<D>;
-    constexpr int TW = kWideRows / (kPgWaves * 32);
+    constexpr int TW = 1, KEYS = kWideTile / WAVES, LOADS = wide_loads<D>();
+    static_assert(WAVES * 32 == kWideRows && KEYS * WAVES == kWideTile && KEYS <= kPgGroup && KEYS == LOADS * X::RPI, "a row tile and some keys of a tile for every wavefront");
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;  // bytes
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     const int ln = lane & 31, hh = lane >> 5;
@@ -756,7 +767,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     const int keys = max(0, before + quot(g.row0 + g.nrows - 1, p.d_g) + 1);
     const int first_lim = before + quot(min(g.row0 + wave * 32, g.row0 + g.nrows - 1), p.d_g) + 1;  // what all rows of the wavefront see
     const int v_row = lane / X::LPR, v_slot = lane % X::LPR;
-    // Lane i knows of tile ahead_from + i: where the wavefront's 16 keys lie, how many bytes of them there are (none without a page, and behind
+    // Lane i knows of tile ahead_from + i: where the wavefront's keys lie, how many bytes of them there are (none without a page, and behind
     // the last key), and which of the tile's four groups have a page.
     unsigned ahead_lo = 0, ahead_hi = 0, ahead_bytes = 0;
     int ahead_have = 0, ahead_from = 0;
@@ -768,17 +779,18 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         for (int i = 0; i < kWideTile / kPgGroup; ++i) {
             const int e = page_entry(p, row, kb + i * kPgGroup);
             if ((unsigned)e < (unsigned)p.pages) ahead_have |= 1 << i;
-            if (i == wave) {
-                const long long at = group_at(p, e, kb + i * kPgGroup, g.kvh);
+            if (i == wave * KEYS / kPgGroup) {
+                const int key = kb + wave * KEYS;
+                const long long at = group_at(p, e, key, g.kvh);
                 ahead_lo = (unsigned)at;
                 ahead_hi = (unsigned)(at >> 32);
-                ahead_bytes = group_bytes(p, e, kb + i * kPgGroup, keys, D * 2);
+                ahead_bytes = group_bytes(p, e, key, min(keys, key + KEYS), D * 2);
             }
         }
     };
     const unsigned row_off = (unsigned)v_row * (unsigned)p.page_t;
-    unsigned piece = (v_slot ^ spread<D>(v_row)) * 16;  // of the first load; the others' differ in the bits that spread() takes from the row's upper part
-    const unsigned to = lds_address(lds) + wave * kPgGroup * ROW;
+    unsigned piece = (v_slot ^ spread<D>(wave * KEYS + v_row)) * 16;  // of the first load; the others' differ in the bits that spread() takes from the row's upper part
+    const unsigned to = lds_address(lds) + wave * KEYS * ROW;
     int have_0 = 0, have_1 = 0;  // of the tile that arrives next and of the one behind it
     const unsigned long long k_to_v = (unsigned long long)p.V - (unsigned long long)p.K;
     unsigned long long at = 0;
@@ -804,14 +816,14 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 #pragma unroll
         for (int v = 0; v < 2; ++v)
 #pragma unroll
-            for (int i = 0; i < X::NLD; ++i) request(g.lo + tile, v, i);
+            for (int i = 0; i < LOADS; ++i) request(g.lo + tile, v, i);
         if (tile == 0) have_0 = have_1;
     }
     // The next tile is in LDS for everybody; everybody has left the tile before the last behind, whose stage the next requests take.  Loads behind
     // the tile's that are on their way: K and V of the next one at first, then K and half of V of the next one.
     auto arrive_tile = [&](bool first) {
-        if (first) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * X::NLD) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(X::NLD + X::NLD / 2) : "memory");
+        if (first) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS + LOADS / 2) : "memory");
         const int have = have_0;
         have_0 = have_1;
         return have;
@@ -820,7 +832,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     int lim[TW];
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
-        const int r = min(g.row0 + (wave + t * kPgWaves) * 32 + ln, g.row0 + g.nrows - 1), i = quot(r, p.d_g);
+        const int r = min(g.row0 + wave * 32 + ln, g.row0 + g.nrows - 1), i = quot(r, p.d_g);
         lim[t] = before + i + 1;
         const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
 #pragma unroll
@@ -843,22 +855,20 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
             for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
     }
     const int row_tiles = __builtin_amdgcn_readfirstlane((g.nrows + 31) / 32 - wave);  // from this wavefront's first on
-    if (row_tiles > kPgWaves) {
-        wide_rows<D, 2>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
-    } else if (row_tiles > 0) {
-        wide_rows<D, 1>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
+    if (row_tiles > 0) {
+        wide_rows<D, TW>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
     } else {  // no rows: the loads and the meetings alone, in the same order
         arrive_tile(true);
 #pragma unroll
-        for (int i = 0; i < X::NLD; ++i) request(g.lo + 2, 0, i);
+        for (int i = 0; i < LOADS; ++i) request(g.lo + 2, 0, i);
         for (int j = g.lo; j + 1 < g.hi; ++j) {
 #pragma unroll
-            for (int i = 0; i < X::NLD / 2; ++i) request(j + 2, 1, i);
+            for (int i = 0; i < LOADS / 2; ++i) request(j + 2, 1, i);
             arrive_tile(false);
 #pragma unroll
-            for (int i = X::NLD / 2; i < X::NLD; ++i) request(j + 2, 1, i);
+            for (int i = LOADS / 2; i < LOADS; ++i) request(j + 2, 1, i);
 #pragma unroll
-            for (int i = 0; i < X::NLD; ++i) request(j + 3, 0, i);
+            for (int i = 0; i < LOADS; ++i) request(j + 3, 0, i);
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -866,7 +876,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
         const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
-        const int r = (wave + t * kPgWaves) * 32 + ln;
+        const int r = wave * 32 + ln;
         if (r >= g.nrows) continue;
         const unsigned at = (unsigned)part_slot(w, g.w0) * p.part_rows + r;
         if (g.parts > 1) {
@@ -893,15 +903,20 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
             }
         if (p.lse && hh == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (m_run[t] * p.scale_log2 + log2f(l)) * 0.69314718055994530942f;
     }
-    if (g.parts > 1) arrive<D>(p, g, rs, w, sh);
+    if (g.parts > 1) arrive<D, WAVES>(p, g, rs, w, sh);
     __syncthreads();
 }
 
+template <bool WIDE>
+__host__ __device__ constexpr int paged_waves() {
+    return WIDE ? 8 : 4;
+}
 template <int D, int NARROW_TILES, bool WIDE>
-__global__ __launch_bounds__(kPgThreads, !WIDE && NARROW_TILES == 1 ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
+__global__ __launch_bounds__(paged_waves<WIDE>() * kWave, !WIDE && NARROW_TILES == 1 ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
+    constexpr int WAVES = paged_waves<WIDE>();
     constexpr int WIDE_LDS = kStages * kWideTile * 2 * D * 2;
-    __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > Tile<D>::LDS ? WIDE_LDS : Tile<D>::LDS];
-    __shared__ float sh_m[kPgWaves][32], sh_l[kPgWaves][32];
+    __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > WAVES * Tile<D>::SLAB ? WIDE_LDS : WAVES * Tile<D>::SLAB];
+    __shared__ float sh_m[WAVES][32], sh_l[WAVES][32];
     __shared__ int sh;
     const int lane = threadIdx.x & (kWave - 1);
     const int per_xcd = p.workers / kNumXCD;  // neighbours in the sequence share an XCD and with it a KV head's keys in its L2
@@ -951,8 +966,12 @@ __global__ __launch_bounds__(kPgThreads, !WIDE && NARROW_TILES == 1 ? 2 : 1) voi
                 g.w0 = g.lo > 0 ? pieces.worker(tile0) : w;
                 g.parts = (g.hi < g.tiles ? pieces.worker(tile0 + (long long)(g.tiles - 1) * each) : w) - g.w0 + 1;
             }
-            if (narrow) narrow_segment<D, NARROW_TILES>(p, g, w, lds, sh_m, sh_l, &sh);
-            else if (WIDE) wide_segment<D>(p, g, w, lds, &sh);
+            if constexpr (WIDE) {
+                if (narrow) narrow_segment<D, NARROW_TILES, WAVES>(p, g, w, lds, sh_m, sh_l, &sh);
+                else wide_segment<D, WAVES>(p, g, w, lds, &sh);
+            } else {
+                narrow_segment<D, NARROW_TILES, WAVES>(p, g, w, lds, sh_m, sh_l, &sh);
+            }
         }
         within = item_end;
         at = head + within;
@@ -1178,8 +1197,8 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     }
     const dim3 grid((unsigned)pl.workers);
     if (pl.wide) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, true>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, true>), grid, block, s, p);
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, true>), grid, dim3(paged_waves<true>() * kWave), s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, true>), grid, dim3(paged_waves<true>() * kWave), s, p);
     } else if (pl.narrow_tiles == 2) {
         if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, false>), grid, block, s, p);
         else LOTTS_LAUNCH((paged_attn_kernel<128, 2, false>), grid, block, s, p);
