@@ -1,6 +1,6 @@
 """Thin Python binding of liblotts.so: argument marshalling only.  The calls that are shorter on the GPU than in Python
-(verify_attention, verify_attention_noalloc, spec_accept, majority_vote, skinny_gemm) go through the extension _calls, the others
-through ctypes.
+(verify_attention, verify_attention_noalloc, spec_accept, majority_vote, skinny_gemm, the paged cache's) go through the extension _calls, the
+others through ctypes.
 
 torch supplies device memory and the current stream; every step of the verify path runs in
 the library's HIP kernels.  There is no fallback: if the library is missing the import fails.
@@ -138,6 +138,9 @@ def load() -> ctypes.CDLL:
         lib.calls = _calls.Calls(*(ctypes.cast(f, vp).value for f in (
             lib.verify_attention_workspace_bytes, lib.verify_attention, lib.spec_accept_workspace_bytes, lib.spec_accept,
             lib.majority_vote, lib.skinny_gemm_workspace_bytes, lib.skinny_gemm, lib.verify_attention_noalloc)))
+        lib.paged = _calls.PagedCalls(*(ctypes.cast(f, vp).value for f in (
+            lib.verify_attention_paged_workspace_bytes, lib.verify_attention_paged, lib.kv_append_paged, lib.kv_pages_reserve, lib.kv_pages_fork,
+            lib.kv_pages_free, lib.kv_pages_compact, lib.kv_pages_copy)))
         _lib = lib
     return _lib
 
@@ -479,63 +482,11 @@ def kv_append(Knew: torch.Tensor, Vnew: torch.Tensor, Kpriv: torch.Tensor, Vpriv
         raise LottsError(rc, "kv_append")
 
 
-def _paged_dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
-        return LOTTS_BF16
-    if t.dtype == torch.float32:
-        return LOTTS_F32
-    raise TypeError("Q, K and V must be bfloat16 or float32")
-
-
-def _on_this_gpu(where: str, *tensors: Optional[torch.Tensor]) -> None:
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != torch._C._cuda_getDevice()):
-            raise ValueError("%s runs on the current GPU, and all its tensors lie there" % where)
-
-
-def _whole_numbers(t: torch.Tensor, numel: int, what: str) -> None:
-    if t.dtype != torch.int32 or not t.is_contiguous():
-        raise TypeError("%s must be contiguous int32" % what)
-    if t.numel() < numel:
-        raise ValueError("%s must hold %d numbers" % (what, numel))
-
-
-def _table(page_table: torch.Tensor) -> Tuple[int, int]:
-    if page_table.dtype != torch.int32:
-        raise TypeError("page_table must be int32")
-    if page_table.dim() != 2 or page_table.stride(1) != 1 or (page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]):
-        raise ValueError("page_table must be [B][columns] with rows apart")
-    return page_table.shape[0], page_table.shape[1]
-
-
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-def _rows_apart(t: torch.Tensor, what: str) -> None:
-    if t.stride(-1) != 1:
-        raise ValueError("%s: the head dimension must be contiguous" % what)
-    if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
-        raise ValueError("%s: expanded tensors are not supported" % what)
-
-
-def _tokens(t: torch.Tensor, B: int, uniform: bool, what: str) -> torch.Tensor:
-    """[T][H][D], from that or from [B][n][H][D] whose tokens lie evenly apart."""
-    if t.dim() == 4 and uniform:
-        if t.shape[0] != B or (t.shape[0] > 1 and t.stride(0) != t.shape[1] * t.stride(1)):
-            raise ValueError("%s [B][n][H][D]: its tokens must lie evenly apart" % what)
-        return t.flatten(0, 1) if t.is_contiguous() else t.as_strided((B * t.shape[1],) + t.shape[2:], t.stride()[1:])
-    if t.dim() != 3:
-        raise ValueError("%s must be [T][H][D]%s" % (what, " or [B][n][H][D]" if uniform else ""))
-    return t
-
-
-def _pages(Kpages: torch.Tensor, Vpages: torch.Tensor) -> None:
-    if Kpages.dim() != 4 or Vpages.shape != Kpages.shape or Vpages.stride() != Kpages.stride():
-        raise ValueError("Kpages and Vpages must be [pages][Hkv][page_tokens][D] with shared strides")
-    if Vpages.dtype != Kpages.dtype:
-        raise TypeError("Kpages and Vpages share one dtype")
-    _rows_apart(Kpages, "Kpages")
+def _current_gpu(where: str, t: torch.Tensor) -> int:
+    """The current device's number; the paged calls' tensors all lie there."""
+    if not t.is_cuda:
+        raise ValueError("%s runs on the GPU only" % where)
+    return torch._C._cuda_getDevice()
 
 
 def verify_attention_paged(Q: torch.Tensor, Kpages: torch.Tensor, Vpages: torch.Tensor, page_table: torch.Tensor, kv_len: torch.Tensor,
@@ -547,42 +498,17 @@ def verify_attention_paged(Q: torch.Tensor, Kpages: torch.Tensor, Vpages: torch.
     may then be [B][n][Hq][D] too.  max_new: the most new tokens of a branch, as far as the caller knows (T if not).
     Returns O of Q's shape and dtype, and LSE [T][Hq] fp32 if asked."""
     lib = load()
-    _on_this_gpu("verify_attention_paged", Q, Kpages, Vpages, page_table, kv_len, q_start, out, lse, workspace)
-    B, columns = _table(page_table)
-    _pages(Kpages, Vpages)
-    q = _tokens(Q, B, q_start is None, "Q")
-    T, Hq, D = q.shape
-    _rows_apart(q, "Q")
+    device, handle = _current_gpu("verify_attention_paged", Q), _stream_handle(stream)
     if out is None:
         out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-    o = _tokens(out, B, q_start is None, "out")
-    _rows_apart(o, "out")
-    if o.shape != q.shape:
-        raise ValueError("out must have Q's shape")
-    if not (Kpages.dtype == out.dtype == Q.dtype):
-        raise TypeError("Q, K, V and out share one dtype")
-    if Kpages.shape[3] != D:
-        raise ValueError("Q and Kpages disagree")
-    _whole_numbers(kv_len, B, "kv_len [B]")
-    if q_start is not None:
-        _whole_numbers(q_start, B + 1, "q_start [B+1]")
-    elif max_new is not None and max_new * B != T:
-        raise ValueError("without q_start every branch has T / B new tokens")
     if return_lse and lse is None:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=Q.device)
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.numel() < T * Hq):
-        raise TypeError("lse must be contiguous float32 [T][Hq]")
-    d = PagedDesc(B, T, (T if q_start is not None else max(1, T // B)) if max_new is None else max_new, Hq, Kpages.shape[1], D, Kpages.shape[2],
-                  Kpages.shape[0], columns, _paged_dtype(Q), float(scale), q.stride(0), q.stride(1), Kpages.stride(0), Kpages.stride(1),
-                  Kpages.stride(2), _row_stride(page_table), o.stride(0), o.stride(1))
-    need = lib.verify_attention_paged_workspace_bytes(ctypes.byref(d))
-    if need == 0:
-        raise LottsError(-2, "verify_attention_paged_workspace_bytes")
-    ws = _workspace("attn_paged", Q.get_device(), need, stream) if workspace is None else workspace
-    rc = lib.verify_attention_paged(ctypes.byref(d), _ptr(Q), _ptr(Kpages), _ptr(Vpages), _ptr(page_table), _ptr(kv_len), _ptr(q_start), _ptr(out),
-                                    _ptr(lse), _ptr(ws), ws.nbytes, _stream_handle(stream))
+        lse = torch.empty((Q.numel() // max(1, Q.shape[-1] * Q.shape[-2]), Q.shape[-2]), dtype=torch.float32, device=Q.device)
+    cached = None if workspace is not None else _workspaces.get(_workspace_key("attn_paged", device, stream))
+    call = lib.paged.verify_attention_paged
+    rc = call(Q, Kpages, Vpages, page_table, kv_len, q_start, max_new, scale, out, lse, workspace, cached, device, handle)
     if rc != 0:
-        raise LottsError(rc, "verify_attention_paged")
+        _finish(rc, "attn_paged", device, stream, lambda ws: call(Q, Kpages, Vpages, page_table, kv_len, q_start, max_new, scale, out, lse, None, ws,
+                                                                  device, handle), "verify_attention_paged")
     return (out, lse) if return_lse else out
 
 
@@ -591,35 +517,9 @@ def kv_append_paged(Knew: torch.Tensor, Vnew: torch.Tensor, Kpages: torch.Tensor
     """Knew/Vnew [T][Hkv][D] (views are fine: only D has to be contiguous, V with K's strides; [B][n][Hkv][D] without q_start) go to the last
     places of their branches, kv_len [B] counting them, in Kpages/Vpages [pages][Hkv][page_tokens][D] (in place)."""
     lib = load()
-    _on_this_gpu("kv_append_paged", Knew, Vnew, Kpages, Vpages, page_table, kv_len, q_start)
-    B, columns = _table(page_table)
-    _pages(Kpages, Vpages)
-    if Vnew.shape != Knew.shape or Vnew.stride() != Knew.stride():
-        raise ValueError("Knew and Vnew must share shape and strides")
-    k = _tokens(Knew, B, q_start is None, "Knew")
-    T, Hkv, D = k.shape
-    _rows_apart(k, "Knew")
-    if not (Vnew.dtype == Kpages.dtype == Knew.dtype):
-        raise TypeError("all four buffers share one dtype")
-    if Kpages.shape[1] != Hkv or Kpages.shape[3] != D:
-        raise ValueError("Knew and Kpages disagree")
-    _whole_numbers(kv_len, B, "kv_len [B]")
-    if q_start is not None:
-        _whole_numbers(q_start, B + 1, "q_start [B+1]")
-    rc = lib.kv_append_paged(B, T, Hkv, D, Kpages.shape[2], Kpages.shape[0], columns, _paged_dtype(Knew), _ptr(Knew), _ptr(Vnew), k.stride(0),
-                             k.stride(1), _ptr(Kpages), _ptr(Vpages), Kpages.stride(0), Kpages.stride(1), Kpages.stride(2), _ptr(page_table),
-                             _row_stride(page_table), _ptr(kv_len), _ptr(q_start), _stream_handle(stream))
+    rc = lib.paged.kv_append_paged(Knew, Vnew, Kpages, Vpages, page_table, kv_len, q_start, _current_gpu("kv_append_paged", Knew), _stream_handle(stream))
     if rc != 0:
         raise LottsError(rc, "kv_append_paged")
-
-
-def _upkeep(where: str, page_table: torch.Tensor, refs: torch.Tensor, kv_len: Optional[torch.Tensor], *others: Optional[torch.Tensor]):
-    _on_this_gpu(where, page_table, refs, kv_len, *others)
-    B, columns = _table(page_table)
-    _whole_numbers(refs, 1, "refs [pages]")
-    if kv_len is not None:
-        _whole_numbers(kv_len, B, "kv_len [B]")
-    return B, columns, refs.numel()
 
 
 def kv_pages_reserve(page_table: torch.Tensor, refs: torch.Tensor, kv_len: torch.Tensor, new_tokens: torch.Tensor, page_tokens: int, *,
@@ -629,19 +529,17 @@ def kv_pages_reserve(page_table: torch.Tensor, refs: torch.Tensor, kv_len: torch
     int32 and changed in place.  Returns (copies [B][2], missing [1]) int32: the shared pages to copy (for kv_pages_copy), and 0, or why
     nothing has been changed (the number of pages lacking; -1: the table is too narrow)."""
     lib = load()
-    B, columns, pages = _upkeep("kv_pages_reserve", page_table, refs, kv_len, new_tokens, copies, missing, workspace)
-    _whole_numbers(new_tokens, B, "new_tokens [B]")
+    device, handle = _current_gpu("kv_pages_reserve", refs), _stream_handle(stream)
     if copies is None:
-        copies = torch.empty((B, 2), dtype=torch.int32, device=refs.device)
+        copies = torch.empty((page_table.shape[0], 2), dtype=torch.int32, device=refs.device)
     if missing is None:
         missing = torch.empty((1,), dtype=torch.int32, device=refs.device)
-    _whole_numbers(copies, 2 * B, "copies [B][2]")
-    _whole_numbers(missing, 1, "missing [1]")
-    ws = _workspace("kv_pages", refs.get_device(), 4 * pages, stream) if workspace is None else workspace
-    rc = lib.kv_pages_reserve(B, columns, pages, int(page_tokens), _ptr(page_table), _row_stride(page_table), _ptr(refs), _ptr(kv_len), _ptr(new_tokens),
-                              _ptr(copies), _ptr(missing), _ptr(ws), ws.nbytes, _stream_handle(stream))
+    cached = None if workspace is not None else _workspaces.get(_workspace_key("kv_pages", device, stream))
+    call = lib.paged.kv_pages_reserve
+    rc = call(page_table, refs, kv_len, new_tokens, page_tokens, copies, missing, workspace, cached, device, handle)
     if rc != 0:
-        raise LottsError(rc, "kv_pages_reserve")
+        _finish(rc, "kv_pages", device, stream, lambda ws: call(page_table, refs, kv_len, new_tokens, page_tokens, copies, missing, None, ws, device, handle),
+                "kv_pages_reserve")
     return copies, missing
 
 
@@ -649,9 +547,7 @@ def kv_pages_fork(page_table: torch.Tensor, refs: torch.Tensor, kv_len: torch.Te
                   stream: Optional[torch.cuda.Stream] = None) -> None:
     """Branch b becomes what branch parent[b] was (b itself: nothing changes; negative: it is emptied); page_table, refs and kv_len in place."""
     lib = load()
-    B, columns, pages = _upkeep("kv_pages_fork", page_table, refs, kv_len, parent)
-    _whole_numbers(parent, B, "parent [B]")
-    rc = lib.kv_pages_fork(B, columns, pages, _ptr(page_table), _row_stride(page_table), _ptr(refs), _ptr(kv_len), _ptr(parent), _stream_handle(stream))
+    rc = lib.paged.kv_pages_fork(page_table, refs, kv_len, parent, _current_gpu("kv_pages_fork", refs), _stream_handle(stream))
     if rc != 0:
         raise LottsError(rc, "kv_pages_fork")
 
@@ -660,11 +556,7 @@ def kv_pages_free(page_table: torch.Tensor, refs: torch.Tensor, kv_len: torch.Te
                   stream: Optional[torch.cuda.Stream] = None) -> None:
     """Branch b is cut to keep[b] tokens (None: to kv_len[b]; 0 ends it) and gives up the pages behind them; in place."""
     lib = load()
-    B, columns, pages = _upkeep("kv_pages_free", page_table, refs, kv_len, keep)
-    if keep is not None:
-        _whole_numbers(keep, B, "keep [B]")
-    rc = lib.kv_pages_free(B, columns, pages, int(page_tokens), _ptr(page_table), _row_stride(page_table), _ptr(refs), _ptr(kv_len), _ptr(keep),
-                           _stream_handle(stream))
+    rc = lib.paged.kv_pages_free(page_table, refs, kv_len, page_tokens, keep, _current_gpu("kv_pages_free", refs), _stream_handle(stream))
     if rc != 0:
         raise LottsError(rc, "kv_pages_free")
 
@@ -674,18 +566,16 @@ def kv_pages_compact(page_table: torch.Tensor, refs: torch.Tensor, *, moves: Opt
     """The n pages in use become pages 0 .. n-1; page_table and refs in place.  Returns (moves [max(1, pages / 2)][2], counts [2] = number of
     moves, n) int32; the data follow by kv_pages_copy(pool, moves, count=counts)."""
     lib = load()
-    B, columns, pages = _upkeep("kv_pages_compact", page_table, refs, None, moves, counts, workspace)
+    device, handle = _current_gpu("kv_pages_compact", refs), _stream_handle(stream)
     if moves is None:
-        moves = torch.empty((max(1, pages // 2), 2), dtype=torch.int32, device=refs.device)
+        moves = torch.empty((max(1, refs.numel() // 2), 2), dtype=torch.int32, device=refs.device)
     if counts is None:
         counts = torch.empty((2,), dtype=torch.int32, device=refs.device)
-    _whole_numbers(moves, 2 * max(1, pages // 2), "moves [max(1, pages / 2)][2]")
-    _whole_numbers(counts, 2, "counts [2]")
-    ws = _workspace("kv_pages", refs.get_device(), 4 * pages, stream) if workspace is None else workspace
-    rc = lib.kv_pages_compact(B, columns, pages, _ptr(page_table), _row_stride(page_table), _ptr(refs), _ptr(moves), _ptr(counts), _ptr(ws), ws.nbytes,
-                              _stream_handle(stream))
+    cached = None if workspace is not None else _workspaces.get(_workspace_key("kv_pages", device, stream))
+    call = lib.paged.kv_pages_compact
+    rc = call(page_table, refs, moves, counts, workspace, cached, device, handle)
     if rc != 0:
-        raise LottsError(rc, "kv_pages_compact")
+        _finish(rc, "kv_pages", device, stream, lambda ws: call(page_table, refs, moves, counts, None, ws, device, handle), "kv_pages_compact")
     return moves, counts
 
 
@@ -693,20 +583,7 @@ def kv_pages_copy(pool: torch.Tensor, pairs: torch.Tensor, *, count: Optional[to
     """Copies pages pairs[j][0] to pairs[j][1] (int32 [n][2]; the first count[0] of them if count is given, numbers that are no page are skipped) in
     every plane of pool [planes][pages][...], whose pages are dense."""
     lib = load()
-    _on_this_gpu("kv_pages_copy", pool, pairs, count)
-    if pool.dim() < 3 or any(n == 0 for n in pool.shape) or not pool[0, 0].is_contiguous():
-        raise ValueError("pool must be [planes][pages][...] with dense pages")
-    if any(n > 1 and s == 0 for n, s in zip(pool.shape, pool.stride())):
-        raise ValueError("expanded tensors are not supported")
-    if pairs.dim() != 2 or pairs.shape[1] != 2:
-        raise ValueError("pairs must be [n][2]")
-    _whole_numbers(pairs, 2, "pairs [n][2]")
-    if count is not None:
-        _whole_numbers(count, 1, "count")
-    size = pool.element_size()
-    page_bytes = pool[0, 0].numel() * size
-    rc = lib.kv_pages_copy(_ptr(pool), pool.shape[0], pool.shape[1], pool.stride(0) * size, pool.stride(1) * size if pool.shape[1] > 1 else page_bytes,
-                           page_bytes, _ptr(pairs), pairs.shape[0], _ptr(count), _stream_handle(stream))
+    rc = lib.paged.kv_pages_copy(pool, pairs, count, _current_gpu("kv_pages_copy", pool), _stream_handle(stream))
     if rc != 0:
         raise LottsError(rc, "kv_pages_copy")
 

@@ -1,10 +1,11 @@
 // The host side of the calls that are shorter on the GPU than in Python: argument checks, the descriptor and the library call of
-// verify_attention (and its _noalloc form), spec_accept, majority_vote and skinny_gemm, as a CPython extension on torch's tensors.  binding.py keeps
+// verify_attention (and its _noalloc form), spec_accept, majority_vote and skinny_gemm, and of the paged cache's calls, as a CPython extension on torch's tensors.  binding.py keeps
 // the signatures, makes what a caller leaves out and holds the workspaces; a call that finds its workspace missing or too small
 // says how much it needs and is made again.
 // Measured (2 branches, fp32, vocabulary 1000): a step's three calls through ctypes are 6.5 + 6.5 + 4.1 us of host time for
 // three launches of 2.7 us each, and their kernels take 11 us together; through here 4.1 + 4.0 + 3.4 us, the step 16.7 -> 12.7.
 #include <Python.h>
+#include <algorithm>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "lotts.h"
@@ -308,6 +309,317 @@ PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
     return reinterpret_cast<PyObject*>(c);
 }
 
+// ---- the paged cache ----------------------------------------------------------------------------------------------------
+using paged_ws_fn = decltype(&verify_attention_paged_workspace_bytes);
+using paged_fn = decltype(&verify_attention_paged);
+using append_fn = decltype(&kv_append_paged);
+using reserve_fn = decltype(&kv_pages_reserve);
+using fork_fn = decltype(&kv_pages_fork);
+using free_fn = decltype(&kv_pages_free);
+using compact_fn = decltype(&kv_pages_compact);
+using copy_fn = decltype(&kv_pages_copy);
+
+struct PagedCalls {
+    PyObject_HEAD
+    paged_ws_fn attn_ws;
+    paged_fn attn;
+    append_fn append;
+    reserve_fn reserve;
+    fork_fn fork;
+    free_fn release;
+    compact_fn compact;
+    copy_fn copy;
+};
+
+// The tensors of a call lie on one GPU, the first one's, and it is the current one (`device`, negative: not looked at).
+struct OneDevice {
+    long device;
+    const at::Tensor& operator()(PyObject* o, const char* what) const {
+        const at::Tensor& t = tensor(o, what);
+        if (device >= 0 && (!t.is_cuda() || t.get_device() != device)) throw Error{PyExc_ValueError, "all tensors lie on the current GPU"};
+        return t;
+    }
+};
+long device_of(PyObject* o) {
+    const long d = PyLong_AsLong(o);
+    if (d == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Error{PyExc_TypeError, "the device must be a number"};
+    }
+    return d;
+}
+// Whole numbers: dense, at least n of them.
+int32_t* numbers(const at::Tensor& t, int64_t n, const char* what) {
+    if (!is(t, at::kInt)) throw Error{PyExc_TypeError, what};
+    if (t.numel() < n) throw Error{PyExc_ValueError, what};
+    return static_cast<int32_t*>(t.data_ptr());
+}
+struct Table {
+    int32_t *entries, B, columns;
+    int64_t stride;
+};
+Table table_of(const at::Tensor& t) {
+    if (t.scalar_type() != at::kInt) throw Error{PyExc_TypeError, "page_table must be int32"};
+    if (t.dim() != 2 || t.stride(1) != 1 || (t.size(0) > 1 && t.stride(0) < t.size(1))) throw Error{PyExc_ValueError, "page_table must be [B][columns] with rows apart"};
+    return {static_cast<int32_t*>(t.data_ptr()), (int32_t)t.size(0), (int32_t)t.size(1), t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), t.size(1))};
+}
+int32_t paged_dtype(const at::Tensor& t) {
+    if (t.scalar_type() == at::kBFloat16) return LOTTS_BF16;
+    if (t.scalar_type() == at::kFloat) return LOTTS_F32;
+    throw Error{PyExc_TypeError, "Q, K and V must be bfloat16 or float32"};
+}
+void rows_apart(const at::Tensor& t) {
+    if (t.strides().back() != 1) throw Error{PyExc_ValueError, "the head dimension must be contiguous"};
+    if (expanded(t)) throw Error{PyExc_ValueError, "expanded tensors are not supported"};
+}
+void same_pages(const at::Tensor& K, const at::Tensor& V) {
+    if (K.dim() != 4 || V.sizes() != K.sizes() || V.strides() != K.strides())
+        throw Error{PyExc_ValueError, "Kpages and Vpages must be [pages][Hkv][page_tokens][D] with shared strides"};
+    if (V.scalar_type() != K.scalar_type()) throw Error{PyExc_TypeError, "Kpages and Vpages share one dtype"};
+    rows_apart(K);
+}
+// Rows of tokens: [T][H][D], or [B][n][H][D] whose tokens lie evenly apart where every branch has as many.
+struct Tokens {
+    int64_t T, H, D, stride_t, stride_h;
+};
+Tokens tokens_of(const at::Tensor& t, int64_t B, bool uniform) {
+    if (t.dim() == 4 && uniform) {
+        if (t.size(0) != B || (B > 1 && t.size(1) > 0 && t.stride(0) != t.size(1) * t.stride(1))) throw Error{PyExc_ValueError, "[B][n][H][D]: the tokens must lie evenly apart"};
+        rows_apart(t);
+        return {B * t.size(1), t.size(2), t.size(3), t.size(1) > 1 ? t.stride(1) : t.stride(0), t.stride(2)};
+    }
+    if (t.dim() != 3) throw Error{PyExc_ValueError, uniform ? "rows of tokens must be [T][H][D] or [B][n][H][D]" : "rows of tokens must be [T][H][D]"};
+    rows_apart(t);
+    return {t.size(0), t.size(1), t.size(2), t.stride(0), t.stride(1)};
+}
+int64_t pitch(int64_t n, int64_t stride, int64_t dense) { return n > 1 ? stride : std::max(stride, dense); }
+
+// Q, Kpages, Vpages, page_table, kv_len, q_start, max_new, scale, out, lse, workspace, cached workspace, device, stream
+PyObject* call_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 14);
+        const OneDevice on{device_of(a[12])};
+        const at::Tensor &Q = on(a[0], "Q must be a tensor"), &K = on(a[1], "Kpages must be a tensor"), &V = on(a[2], "Vpages must be a tensor"),
+                         &table = on(a[3], "page_table must be a tensor"), &len = on(a[4], "kv_len must be a tensor"), &O = on(a[8], "out must be a tensor");
+        const bool uniform = a[5] == Py_None;
+        const Table tab = table_of(table);
+        same_pages(K, V);
+        const Tokens q = tokens_of(Q, tab.B, uniform), o = tokens_of(O, tab.B, uniform);
+        if (O.sizes() != Q.sizes()) throw Error{PyExc_ValueError, "out must have Q's shape"};
+        if (K.scalar_type() != Q.scalar_type() || O.scalar_type() != Q.scalar_type()) throw Error{PyExc_TypeError, "Q, K, V and out share one dtype"};
+        if (K.size(3) != q.D) throw Error{PyExc_ValueError, "Q and Kpages disagree"};
+        if (q.T > 0x7fffffff) throw Error{PyExc_ValueError, "too many tokens"};
+        const int32_t* lens = numbers(len, tab.B, "kv_len must be contiguous int32 [B]");
+        const int32_t* start = uniform ? nullptr : numbers(on(a[5], "q_start must be a tensor"), (int64_t)tab.B + 1, "q_start must be contiguous int32 [B+1]");
+        long most = a[6] == Py_None ? (uniform ? std::max<long>(1, q.T / std::max(1, tab.B)) : (long)q.T) : PyLong_AsLong(a[6]);
+        const double scale = PyFloat_AsDouble(a[7]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            throw Error{PyExc_TypeError, "max_new and scale must be numbers"};
+        }
+        if (most < 0 || most > 0x7fffffff) most = 0;
+        if (uniform && most * tab.B != q.T) throw Error{PyExc_ValueError, "without q_start every branch has T / B new tokens"};
+        float* lse = nullptr;
+        if (a[9] != Py_None) {
+            on(a[9], "lse must be a tensor");
+            lse = rows_of<float>(a[9], at::kFloat, q.T * q.H, "lse must be contiguous float32 [T][Hq]");
+        }
+        lotts_paged_desc d = {tab.B, (int32_t)q.T, (int32_t)most, (int32_t)q.H, (int32_t)K.size(1), (int32_t)q.D, (int32_t)K.size(2), (int32_t)K.size(0), tab.columns,
+                              paged_dtype(Q), (float)scale, pitch(q.T, q.stride_t, q.H * q.D), pitch(q.H, q.stride_h, q.D), K.stride(0), K.stride(1),
+                              pitch(K.size(2), K.stride(2), q.D), tab.stride, pitch(o.T, o.stride_t, q.H * q.D), pitch(o.H, o.stride_h, q.D)};
+        const size_t need = c->attn_ws(&d);
+        if (need == 0) return kNoWorkspaceQuery;
+        void* ws;
+        size_t bytes;
+        if (a[10] != Py_None) on(a[10], "the workspace must be a tensor");
+        if (!workspace(a[10], a[11], need, &ws, &bytes)) return (Py_ssize_t)need;
+        const void *qp = Q.data_ptr(), *kp = K.data_ptr(), *vp = V.data_ptr();
+        void *op = O.data_ptr(), *stream = address(a[13]);
+        return released([&] { return c->attn(&d, qp, kp, vp, tab.entries, lens, start, op, lse, ws, bytes, stream); });
+    });
+}
+
+// Knew, Vnew, Kpages, Vpages, page_table, kv_len, q_start, device, stream
+PyObject* call_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 9);
+        const OneDevice on{device_of(a[7])};
+        const at::Tensor &Kn = on(a[0], "Knew must be a tensor"), &Vn = on(a[1], "Vnew must be a tensor"), &K = on(a[2], "Kpages must be a tensor"),
+                         &V = on(a[3], "Vpages must be a tensor"), &table = on(a[4], "page_table must be a tensor"), &len = on(a[5], "kv_len must be a tensor");
+        const bool uniform = a[6] == Py_None;
+        const Table tab = table_of(table);
+        same_pages(K, V);
+        if (Vn.sizes() != Kn.sizes() || Vn.strides() != Kn.strides()) throw Error{PyExc_ValueError, "Knew and Vnew must share shape and strides"};
+        const Tokens k = tokens_of(Kn, tab.B, uniform);
+        if (Vn.scalar_type() != Kn.scalar_type() || K.scalar_type() != Kn.scalar_type()) throw Error{PyExc_TypeError, "all four buffers share one dtype"};
+        if (K.size(1) != k.H || K.size(3) != k.D) throw Error{PyExc_ValueError, "Knew and Kpages disagree"};
+        if (k.T > 0x7fffffff) throw Error{PyExc_ValueError, "too many tokens"};
+        const int32_t* lens = numbers(len, tab.B, "kv_len must be contiguous int32 [B]");
+        const int32_t* start = uniform ? nullptr : numbers(on(a[6], "q_start must be a tensor"), (int64_t)tab.B + 1, "q_start must be contiguous int32 [B+1]");
+        const void *kn = Kn.data_ptr(), *vn = Vn.data_ptr();
+        void *kp = K.data_ptr(), *vp = V.data_ptr(), *stream = address(a[8]);
+        const lotts_dtype dt = (lotts_dtype)paged_dtype(Kn);
+        return released([&] {
+            return c->append(tab.B, (int32_t)k.T, (int32_t)k.H, (int32_t)k.D, (int32_t)K.size(2), (int32_t)K.size(0), tab.columns, dt, kn, vn, k.stride_t,
+                             pitch(k.H, k.stride_h, k.D), kp, vp, K.stride(0), K.stride(1), pitch(K.size(2), K.stride(2), k.D), tab.entries, tab.stride, lens, start, stream);
+        });
+    });
+}
+
+struct Upkeep {
+    Table tab;
+    int32_t *refs, pages;
+};
+Upkeep upkeep_of(const OneDevice& on, PyObject* table, PyObject* refs) {
+    Upkeep u;
+    u.tab = table_of(on(table, "page_table must be a tensor"));
+    const at::Tensor& r = on(refs, "refs must be a tensor");
+    u.refs = numbers(r, 1, "refs must be contiguous int32 [pages]");
+    if (r.numel() > 0x7fffffff) throw Error{PyExc_ValueError, "too many pages"};
+    u.pages = (int32_t)r.numel();
+    return u;
+}
+
+// page_table, refs, kv_len, new_tokens, page_tokens, copies, missing, workspace, cached workspace, device, stream
+PyObject* call_reserve(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 11);
+        const OneDevice on{device_of(a[9])};
+        const Upkeep u = upkeep_of(on, a[0], a[1]);
+        int32_t* len = numbers(on(a[2], "kv_len must be a tensor"), u.tab.B, "kv_len must be contiguous int32 [B]");
+        const int32_t* more = numbers(on(a[3], "new_tokens must be a tensor"), u.tab.B, "new_tokens must be contiguous int32 [B]");
+        const int32_t page = (int32_t)device_of(a[4]);
+        int32_t* copies = numbers(on(a[5], "copies must be a tensor"), 2 * (int64_t)u.tab.B, "copies must be contiguous int32 [B][2]");
+        int32_t* missing = numbers(on(a[6], "missing must be a tensor"), 1, "missing must be contiguous int32 [1]");
+        const size_t need = 4 * (size_t)u.pages;
+        void* ws;
+        size_t bytes;
+        if (a[7] != Py_None) on(a[7], "the workspace must be a tensor");
+        if (!workspace(a[7], a[8], need, &ws, &bytes)) return (Py_ssize_t)need;
+        void* stream = address(a[10]);
+        return released([&] { return c->reserve(u.tab.B, u.tab.columns, u.pages, page, u.tab.entries, u.tab.stride, u.refs, len, more, copies, missing, ws, bytes, stream); });
+    });
+}
+
+// page_table, refs, kv_len, parent, device, stream
+PyObject* call_fork(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 6);
+        const OneDevice on{device_of(a[4])};
+        const Upkeep u = upkeep_of(on, a[0], a[1]);
+        int32_t* len = numbers(on(a[2], "kv_len must be a tensor"), u.tab.B, "kv_len must be contiguous int32 [B]");
+        const int32_t* parent = numbers(on(a[3], "parent must be a tensor"), u.tab.B, "parent must be contiguous int32 [B]");
+        void* stream = address(a[5]);
+        return released([&] { return c->fork(u.tab.B, u.tab.columns, u.pages, u.tab.entries, u.tab.stride, u.refs, len, parent, stream); });
+    });
+}
+
+// page_table, refs, kv_len, page_tokens, keep, device, stream
+PyObject* call_free(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 7);
+        const OneDevice on{device_of(a[5])};
+        const Upkeep u = upkeep_of(on, a[0], a[1]);
+        int32_t* len = numbers(on(a[2], "kv_len must be a tensor"), u.tab.B, "kv_len must be contiguous int32 [B]");
+        const int32_t page = (int32_t)device_of(a[3]);
+        const int32_t* keep = a[4] == Py_None ? nullptr : numbers(on(a[4], "keep must be a tensor"), u.tab.B, "keep must be contiguous int32 [B]");
+        void* stream = address(a[6]);
+        return released([&] { return c->release(u.tab.B, u.tab.columns, u.pages, page, u.tab.entries, u.tab.stride, u.refs, len, keep, stream); });
+    });
+}
+
+// page_table, refs, moves, counts, workspace, cached workspace, device, stream
+PyObject* call_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 8);
+        const OneDevice on{device_of(a[6])};
+        const Upkeep u = upkeep_of(on, a[0], a[1]);
+        int32_t* moves = numbers(on(a[2], "moves must be a tensor"), 2 * std::max<int64_t>(1, u.pages / 2), "moves must be contiguous int32 [max(1, pages / 2)][2]");
+        int32_t* counts = numbers(on(a[3], "counts must be a tensor"), 2, "counts must be contiguous int32 [2]");
+        const size_t need = 4 * (size_t)u.pages;
+        void* ws;
+        size_t bytes;
+        if (a[4] != Py_None) on(a[4], "the workspace must be a tensor");
+        if (!workspace(a[4], a[5], need, &ws, &bytes)) return (Py_ssize_t)need;
+        void* stream = address(a[7]);
+        return released([&] { return c->compact(u.tab.B, u.tab.columns, u.pages, u.tab.entries, u.tab.stride, u.refs, moves, counts, ws, bytes, stream); });
+    });
+}
+
+// pool, pairs, count, device, stream
+PyObject* call_copy(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 5);
+        const OneDevice on{device_of(a[3])};
+        const at::Tensor &pool = on(a[0], "pool must be a tensor"), &pairs = on(a[1], "pairs must be a tensor");
+        int64_t page = 1;  // elements of a page, dense
+        bool dense = pool.dim() >= 3 && pool.numel() > 0;
+        for (int64_t i = pool.dim() - 1; dense && i >= 2; --i) {
+            dense = pool.size(i) == 1 || pool.stride(i) == page;
+            page *= pool.size(i);
+        }
+        if (!dense) throw Error{PyExc_ValueError, "pool must be [planes][pages][...] with dense pages"};
+        if (expanded(pool)) throw Error{PyExc_ValueError, "expanded tensors are not supported"};
+        if (pairs.dim() != 2 || pairs.size(1) != 2 || pairs.size(0) > 0x7fffffff || pool.size(0) > 0x7fffffff || pool.size(1) > 0x7fffffff)
+            throw Error{PyExc_ValueError, "pairs must be [n][2]"};
+        const int32_t* from_to = numbers(pairs, 2, "pairs must be contiguous int32 [n][2]");
+        const int32_t* count = a[2] == Py_None ? nullptr : numbers(on(a[2], "count must be a tensor"), 1, "count must be contiguous int32");
+        const int64_t size = (int64_t)pool.element_size();
+        void *base = pool.data_ptr(), *stream = address(a[4]);
+        return released([&] {
+            return c->copy(base, (int32_t)pool.size(0), (int32_t)pool.size(1), pool.stride(0) * size, (pool.size(1) > 1 ? pool.stride(1) : page) * size, page * size, from_to,
+                           (int32_t)pairs.size(0), count, stream);
+        });
+    });
+}
+
+// PagedCalls(address of verify_attention_paged_workspace_bytes, verify_attention_paged, kv_append_paged, kv_pages_reserve, kv_pages_fork,
+// kv_pages_free, kv_pages_compact, kv_pages_copy)
+PyObject* paged_new(PyTypeObject* type, PyObject* args, PyObject*) {
+    void* f[8];
+    if (PyTuple_GET_SIZE(args) != 8) {
+        PyErr_SetString(PyExc_TypeError, "eight addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 8; ++i) {
+        f[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(args, i));
+        if (!f[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an address is 0");
+            return nullptr;
+        }
+    }
+    PagedCalls* c = reinterpret_cast<PagedCalls*>(type->tp_alloc(type, 0));
+    if (!c) return nullptr;
+    c->attn_ws = reinterpret_cast<paged_ws_fn>(f[0]);
+    c->attn = reinterpret_cast<paged_fn>(f[1]);
+    c->append = reinterpret_cast<append_fn>(f[2]);
+    c->reserve = reinterpret_cast<reserve_fn>(f[3]);
+    c->fork = reinterpret_cast<fork_fn>(f[4]);
+    c->release = reinterpret_cast<free_fn>(f[5]);
+    c->compact = reinterpret_cast<compact_fn>(f[6]);
+    c->copy = reinterpret_cast<copy_fn>(f[7]);
+    return reinterpret_cast<PyObject*>(c);
+}
+
+PyMethodDef paged_methods[] = {
+    {"verify_attention_paged", (PyCFunction)(void (*)(void))call_paged, METH_FASTCALL, nullptr},
+    {"kv_append_paged", (PyCFunction)(void (*)(void))call_append, METH_FASTCALL, nullptr},
+    {"kv_pages_reserve", (PyCFunction)(void (*)(void))call_reserve, METH_FASTCALL, nullptr},
+    {"kv_pages_fork", (PyCFunction)(void (*)(void))call_fork, METH_FASTCALL, nullptr},
+    {"kv_pages_free", (PyCFunction)(void (*)(void))call_free, METH_FASTCALL, nullptr},
+    {"kv_pages_compact", (PyCFunction)(void (*)(void))call_compact, METH_FASTCALL, nullptr},
+    {"kv_pages_copy", (PyCFunction)(void (*)(void))call_copy, METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject paged_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
 PyMethodDef calls_methods[] = {
     {"verify_attention", (PyCFunction)(void (*)(void))call_attention, METH_FASTCALL, nullptr},
     {"verify_attention_noalloc", (PyCFunction)(void (*)(void))call_attention_noalloc, METH_FASTCALL, nullptr},
@@ -327,14 +639,21 @@ PyMODINIT_FUNC PyInit__calls(void) {
     calls_type.tp_flags = Py_TPFLAGS_DEFAULT;
     calls_type.tp_new = calls_new;
     calls_type.tp_methods = calls_methods;
-    if (PyType_Ready(&calls_type) < 0) return nullptr;
+    paged_type.tp_name = "_calls.PagedCalls";
+    paged_type.tp_basicsize = sizeof(PagedCalls);
+    paged_type.tp_flags = Py_TPFLAGS_DEFAULT;
+    paged_type.tp_new = paged_new;
+    paged_type.tp_methods = paged_methods;
+    if (PyType_Ready(&calls_type) < 0 || PyType_Ready(&paged_type) < 0) return nullptr;
     PyObject* m = PyModule_Create(&calls_module);
     if (!m) return nullptr;
-    Py_INCREF(&calls_type);
-    if (PyModule_AddObject(m, "Calls", reinterpret_cast<PyObject*>(&calls_type)) < 0) {
-        Py_DECREF(&calls_type);
-        Py_DECREF(m);
-        return nullptr;
+    for (PyTypeObject* type : {&calls_type, &paged_type}) {
+        Py_INCREF(type);
+        if (PyModule_AddObject(m, type == &calls_type ? "Calls" : "PagedCalls", reinterpret_cast<PyObject*>(type)) < 0) {
+            Py_DECREF(type);
+            Py_DECREF(m);
+            return nullptr;
+        }
     }
     if (PyModule_AddStringConstant(m, "built_for_torch", LOTTS_TORCH) < 0) {
         Py_DECREF(m);
