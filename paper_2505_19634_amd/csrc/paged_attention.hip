@@ -285,12 +285,13 @@ struct Tile {
     static constexpr int LPR = D / 8;             // lanes per key row of a load
     static constexpr int RPI = kWave / LPR;       // key rows per load instruction
     static constexpr int NLD = kPgGroup / RPI;    // load instructions per 16 keys
-    static constexpr int KSTRIDE = D * 2 + 16;    // bytes per key row in LDS (pad: conflict-free 16-byte row reads)
-    static constexpr int VSTRIDE = D * 2 + 64;    // (pad: conflict-free transposing reads)
     static constexpr int OSTRIDE = D + 4;         // floats per row of a parked output
-    static constexpr int SLAB = kNarrowTile * (KSTRIDE + VSTRIDE);  // LDS of a wavefront (narrow)
-    static_assert(32 * OSTRIDE * 4 <= SLAB, "a parked output reuses the wavefront's slab");
 };
+// LDS of a wavefront with a narrow item: its tiles, and its output when the states meet.
+template <int D>
+__host__ __device__ constexpr int narrow_slab(int stages) {
+    return std::max(stages * kNarrowTile * D * 4, (32 * Tile<D>::OSTRIDE * 4 + 255) / 256 * 256);
+}
 
 // Maximum of a lane's and its partner's 32 lanes away.
 __device__ __forceinline__ float max_halves(float v) {
@@ -329,59 +330,110 @@ __device__ __forceinline__ void softmax_step(f32x16& s, f32x16 (&o)[DB], float& 
     }
 }
 
+// Key tiles get into LDS by the loads themselves, 16 bytes a lane: lane i of a load writes piece i behind
+// the load's base, so rows cannot be padded; instead piece c of row r lies at c ^ spread(r), which the lane that loads it picks.  Both the 16-byte row
+// reads of K (32 rows, one piece) and the transposing reads of V (8 rows, 4 neighbouring pieces) then meet every bank equally often.
 template <int D>
-__device__ __forceinline__ bf16x8 read_v(const unsigned char* at) {
+__device__ __forceinline__ int spread(int r) {
+    if (D == 128) return (r & 3) << 2 | (r >> 2 & 3);  // 16 pieces a row
+    return (r >> 1 & 1) << 2 | (r >> 2 & 3);           // 8 pieces a row, two rows next to each other
+}
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // M0 is on the clobber list on purpose
+template <bool ONCE>  // what is read once passes the caches by
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned off, unsigned lds_base) {
+    if (ONCE) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen nt lds" : : "v"(off), "s"(lds_base), "s"(r) : "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(off), "s"(lds_base), "s"(r) : "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ unsigned lds_address(const void* at) {
+    return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)at);
+}
+
+constexpr int kStages = 4;     // tiles in LDS: one whose V is read, one whose K is read, two on their way
+constexpr float kRescale = 8.f;  // a running maximum may be behind the true one by a factor of 2^8 before the state is rescaled
+
+// Pieces of a tile at an address in LDS, K rows and V rows ROW bytes apart.  (What differs between the pieces of a lane lies in bits of the address that
+// its row does not touch: one register and an exclusive or.)
+template <int D>
+__device__ __forceinline__ unsigned lane_of_k(int lane) {
+    return (lane & 31) * (D * 2) + ((lane >> 5) ^ spread<D>(lane & 15)) * 16;
+}
+template <int D>
+__device__ __forceinline__ bf16x8 read_k(unsigned at, int i) {  // A operand of K Q^T: key lane % 32, the i-th 16 of the head dimension
+    return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(at ^ (i * 32));
+}
+template <int D>
+__device__ __forceinline__ unsigned lane_of_v(int lane) {
+    const int blk = lane >> 4, i16 = lane & 15, r = (blk >> 1) * 4 + (i16 >> 2);
+    return r * (D * 2) + (((blk & 1) * 2 + (i16 >> 1 & 1)) ^ spread<D>(r)) * 16 + (i16 & 1) * 8;
+}
+template <int D>
+__device__ __forceinline__ bf16x8 read_v(unsigned at, int kk, int db) {  // A operand of V^T P^T: 32 columns from 32 db on, the kk-th 16 keys
     union {
         short4v s[2];
         bf16x8 v;
     } f;
-    f.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(at));
-    f.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(at + 8 * Tile<D>::VSTRIDE));
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(uintptr_t)((at ^ (db * 64 + h * 32)) + (kk * 16 + h * 8) * (D * 2)));
     return f.v;
 }
 
-// A narrow item's part: wavefront w takes tiles lo + w, lo + w + WAVES, ..., each into registers one tile ahead and through a slab of its own.
-template <int D, int TW, int WAVES>
+// A narrow item's part: wavefront w takes tiles lo + w, lo + w + WAVES, ..., through STAGES slabs of its own: with two, the next tile is on its way while
+// one is worked on; with one, the other wavefronts' are.
+template <int D, int TW, int WAVES, int STAGES>
 __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh) {
     using X = Tile<D>;
+    constexpr int ROW = D * 2, HALF = kNarrowTile * ROW, SLAB = narrow_slab<D>(STAGES), LOADS = 4 * X::NLD;  // of a tile
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     const int ln = lane & 31, hh = lane >> 5;
     const int32_t* row = p.table + g.b * p.table_stride;
     const int keys = min(g.L, max(0, g.L - g.n + quot(g.nrows - 1, p.d_g) + 1)), before = g.L - g.n;
     const int n_tiles = g.lo + wave < g.hi ? (g.hi - 1 - g.lo - wave) / WAVES + 1 : 0;
-    const int v_row = lane / X::LPR, v_chunk = lane % X::LPR;
-    const int blk = lane >> 4, i16 = lane & 15;
-    const int tr_off = ((blk >> 1) * 4 + (i16 >> 2)) * X::VSTRIDE + ((blk & 1) * 16 + (i16 & 3) * 4) * 2;
-    unsigned char *kslab = lds + wave * X::SLAB, *vslab = kslab + kNarrowTile * X::KSTRIDE;
-    int ahead[2], ahead_from = 0;  // entries of the wavefront's tiles ahead_from .. ahead_from + 63
+    const int v_row = lane / X::LPR, v_slot = lane % X::LPR;
+    const unsigned slab = lds_address(lds) + wave * SLAB, row_off = (unsigned)v_row * (unsigned)p.page_t;
+    const unsigned piece = (v_slot ^ spread<D>(v_row)) * 16;  // of the first load; the others' differ in the bits that spread() takes from the row's upper part
+    // Lane i knows of the wavefront's tile ahead_from + i where its two groups of 16 keys lie and how many bytes of them there are (none
+    // without a page, and behind the last key).
+    unsigned ahead_lo[2], ahead_hi[2], ahead_bytes[2];
+    int ahead_from = 0;
     auto look_ahead = [&](int it) {
         ahead_from = it;
-        const int key = (g.lo + wave + (it + lane) * WAVES) * kNarrowTile;
-        ahead[0] = page_entry(p, row, key);
-        ahead[1] = page_entry(p, row, key + kPgGroup);
-    };
-    u32x4 kst[2][X::NLD], vst[2][X::NLD];
-    int have_next = 0;
-    auto fetch = [&](int it) {
-        if (it - ahead_from >= kWave) look_ahead(it);
-        const int kb = (g.lo + wave + it * WAVES) * kNarrowTile;
-        have_next = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int key = kb + h * kPgGroup, e = __builtin_amdgcn_readlane(ahead[h], it - ahead_from);
-            const unsigned bytes = group_bytes(p, e, key, keys, D * 2);
+            const int key = (g.lo + wave + (it + lane) * WAVES) * kNarrowTile + h * kPgGroup, e = page_entry(p, row, key);
             const long long at = group_at(p, e, key, g.kvh);
-            have_next |= (unsigned)e < (unsigned)p.pages ? 1 << h : 0;
-            const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes), vr = buffer((const unsigned char*)p.V + at, bytes);
-#pragma unroll
-            for (int i = 0; i < X::NLD; ++i) {
-                const unsigned off = (unsigned)(i * X::RPI + v_row) * (unsigned)p.page_t + v_chunk * 16;
-                kst[h][i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (int)off, 0, 2);
-                vst[h][i] = __builtin_amdgcn_raw_buffer_load_b128(vr, (int)off, 0, 2);
-            }
+            ahead_lo[h] = (unsigned)at;
+            ahead_hi[h] = (unsigned)(at >> 32);
+            ahead_bytes[h] = group_bytes(p, e, key, keys, D * 2) | ((unsigned)e < (unsigned)p.pages ? 1u : 0u);  // (a multiple of 16; bit 0: it has a page)
         }
     };
-    if (n_tiles > 0) look_ahead(0);
+    auto fetch = [&](int it) {
+        if (it - ahead_from >= kWave) look_ahead(it);
+        const int x = it - ahead_from;
+        const unsigned stage = slab + (STAGES > 1 ? (it & 1) * 2 * HALF : 0);
+        int have = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const long long at = (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane(ahead_hi[h], x) << 32 | (unsigned)__builtin_amdgcn_readlane(ahead_lo[h], x));
+            const unsigned bytes = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(ahead_bytes[h], x));
+            have |= (int)(bytes & 1) << h;
+            const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes & ~1u), vr = buffer((const unsigned char*)p.V + at, bytes & ~1u);
+#pragma unroll
+            for (int i = 0; i < X::NLD; ++i) {
+                const unsigned off = row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (piece ^ spread<D>(i * X::RPI) * 16);
+                load_to_lds<true>(kr, off, stage + h * kPgGroup * ROW + i * 1024);
+                load_to_lds<true>(vr, off, stage + HALF + h * kPgGroup * ROW + i * 1024);
+            }
+        }
+        return have;
+    };
+    int have_next = 0;
+    if (n_tiles > 0) {
+        look_ahead(0);
+        have_next = fetch(0);
+    }
     bf16x8 qf[TW][X::KS];
     int lim[TW];
 #pragma unroll
@@ -392,8 +444,8 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
 #pragma unroll
         for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
     }
-    if (n_tiles > 0) fetch(0);
     const bool two = TW > 1 && g.nrows > 32;
+    const unsigned kat = slab + lane_of_k<D>(lane), vat = slab + HALF + lane_of_v<D>(lane);
     f32x16 oacc[TW][X::DB];
     float m_run[TW], l_run[TW];
 #pragma unroll
@@ -406,20 +458,19 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
     }
     for (int it = 0; it < n_tiles; ++it) {
-        const int kb = (g.lo + wave + it * WAVES) * kNarrowTile;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < X::NLD; ++i) {
-                *reinterpret_cast<u32x4*>(kslab + (h * kPgGroup + i * X::RPI + v_row) * X::KSTRIDE + v_chunk * 16) = kst[h][i];
-                *reinterpret_cast<u32x4*>(vslab + (h * kPgGroup + i * X::RPI + v_row) * X::VSTRIDE + v_chunk * 16) = vst[h][i];
-            }
-        const int have = have_next;
-        if (it + 1 < n_tiles) fetch(it + 1);
+        const int kb = (g.lo + wave + it * WAVES) * kNarrowTile, have = have_next;
+        const unsigned stage = STAGES > 1 ? (it & 1) * 2 * HALF : 0;
+        if (STAGES > 1 && it + 1 < n_tiles) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile before has been read
+            have_next = fetch(it + 1);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
         const bool masked = have != 3 || kb + kNarrowTile > before + 1;
         bf16x8 kf[X::KS], pf[TW][2];
 #pragma unroll
-        for (int s = 0; s < X::KS; ++s) kf[s] = *reinterpret_cast<const bf16x8*>(kslab + ln * X::KSTRIDE + (2 * s + hh) * 16);
+        for (int s = 0; s < X::KS; ++s) kf[s] = read_k<D>(kat + stage, s);
 #pragma unroll
         for (int t = 0; t < TW; ++t) {
             if (t > 0 && !two) continue;
@@ -434,17 +485,21 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int db = 0; db < X::DB; ++db) {
-                const bf16x8 v = read_v<D>(vslab + tr_off + kk * 16 * X::VSTRIDE + db * 64);
+                const bf16x8 v = read_v<D>(vat + stage, kk, db);
 #pragma unroll
                 for (int t = 0; t < TW; ++t)
                     if (t == 0 || two) oacc[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[t][kk], oacc[t][db], 0, 0, 0);
             }
+        if (STAGES == 1 && it + 1 < n_tiles) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            have_next = fetch(it + 1);
+        }
     }
     // the wavefronts' states of a row tile meet in LDS, in their order
     const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
-    constexpr int F4 = D / 4, QPT = 32 * F4 / (WAVES * kWave), RSTEP = (WAVES * kWave) / F4;
+    constexpr int F4 = D / 4, QPT = 32 * F4 / (WAVES * kWave), RSTEP = WAVES * kWave / F4;
     const int c4 = tid % F4, row0 = tid / F4;
-    float* obuf = reinterpret_cast<float*>(kslab);
+    float* obuf = reinterpret_cast<float*>(lds + wave * SLAB);
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
         if (t > 0 && !two) continue;
@@ -473,7 +528,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
 #pragma unroll
             for (int v = 0; v < WAVES; ++v) {
                 const float f = __builtin_amdgcn_exp2f(sh_m[v][rt] - Mu);
-                const float4 ov = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds + v * X::SLAB) + rt * X::OSTRIDE + c4 * 4);
+                const float4 ov = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds + v * SLAB) + rt * X::OSTRIDE + c4 * 4);
                 sum += sh_l[v][rt] * f;
                 o.x += ov.x * f; o.y += ov.y * f; o.z += ov.z * f; o.w += ov.w * f;
             }
@@ -491,27 +546,6 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
 }
 
 // ---- wide items ----
-// A stage of LDS holds the K and V rows of a tile, 16 bytes a piece, put there by the loads themselves: lane i of a load writes piece i behind
-// the load's base, so rows cannot be padded; instead piece c of row r lies at c ^ spread(r), which the lane that loads it picks.  Both the 16-byte row
-// reads of K (32 rows, one piece) and the transposing reads of V (8 rows, 4 neighbouring pieces) then meet every bank equally often.
-template <int D>
-__device__ __forceinline__ int spread(int r) {
-    if (D == 128) return (r & 3) << 2 | (r >> 2 & 3);  // 16 pieces a row
-    return (r >> 1 & 1) << 2 | (r >> 2 & 3);           // 8 pieces a row, two rows next to each other
-}
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"  // M0 is on the clobber list on purpose
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, unsigned off, unsigned lds_base) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" : : "v"(off), "s"(lds_base), "s"(r) : "m0");
-}
-#pragma clang diagnostic pop
-__device__ __forceinline__ unsigned lds_address(const void* at) {
-    return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)at);
-}
-
-constexpr int kStages = 4;     // tiles in LDS: one whose V is read, one whose K is read, two on their way
-constexpr float kRescale = 8.f;  // a running maximum may be behind the true one by a factor of 2^8 before the state is rescaled
-
 // Loads of a wavefront for its keys of a tile, K or V.
 template <int D>
 __device__ constexpr int wide_loads() {
@@ -556,19 +590,8 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     f32x16 sa[N], sb[N];  // scores as products leave them, in turns: of the keys that are weighed, of the next ones
     bf16x8 pf[N][2];
     const float scale = p.scale_log2, rescale = kRescale / scale;
-    // (What differs between the pieces of a lane lies in bits of the address that its row does not touch: one register and an exclusive or.)
-    auto read_k = [&](unsigned st, int i) { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)((st + kat) ^ (i * 32)); };
-    auto read_v = [&](unsigned st, int i) {
-        union {
-            short4v s[2];
-            bf16x8 v;
-        } f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) short4v*)(uintptr_t)(((st + vat) ^ (i % X::DB * 64 + h * 32)) + HALF + (i / X::DB * 16 + h * 8) * ROW));
-        return f.v;
-    };
+    auto read_k = [&](unsigned st, int i) { return lotts::read_k<D>(st + kat, i); };
+    auto read_v = [&](unsigned st, int i) { return lotts::read_v<D>(st + vat, i / X::DB, i % X::DB); };
     // (Every result is pinned where it is computed: the compiler would move it down to its use, behind the mask's branch.)
     auto scale_pair = [&](f32x16 (&c)[N], int q) {
         const int t = q % N, x = q / N * 2;
@@ -807,7 +830,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         }
         unsigned first = piece;
         asm volatile("" : "+v"(first));  // (formed where it is used: four offsets are three registers more)
-        load_to_lds(buffer((const unsigned char*)p.K + (long long)(at + (k_to_v & (unsigned long long)-(long long)v)), bytes), row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (first ^ spread<D>(i * X::RPI) * 16),
+        load_to_lds<false>(buffer((const unsigned char*)p.K + (long long)(at + (k_to_v & (unsigned long long)-(long long)v)), bytes), row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (first ^ spread<D>(i * X::RPI) * 16),
                     stage + v * HALF + i * 1024);
     };
     look_ahead(g.lo);
@@ -838,11 +861,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 #pragma unroll
         for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
     }
-    // where the lane finds its pieces in a stage
-    const int blk = lane >> 4, i16 = lane & 15;
-    const unsigned lds0 = lds_address(lds), kat = lds0 + ln * ROW + (hh ^ spread<D>(ln & 15)) * 16;
-    const int vr = (blk >> 1) * 4 + (i16 >> 2);
-    const unsigned vat = lds0 + vr * ROW + (((blk & 1) * 2 + (i16 >> 1 & 1)) ^ spread<D>(vr)) * 16 + (i16 & 1) * 8;
+    const unsigned kat = lds_address(lds) + lane_of_k<D>(lane), vat = lds_address(lds) + HALF + lane_of_v<D>(lane);
     f32x16 oacc[TW][X::DB];
     float m_run[TW], l_run[TW];
 #pragma unroll
@@ -912,10 +931,10 @@ __host__ __device__ constexpr int paged_waves() {
     return WIDE ? 8 : 4;
 }
 template <int D, int NARROW_TILES, bool WIDE>
-__global__ __launch_bounds__(paged_waves<WIDE>() * kWave, !WIDE && NARROW_TILES == 1 ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
+__global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel(const PagedParams p) {
     constexpr int WAVES = paged_waves<WIDE>();
-    constexpr int WIDE_LDS = kStages * kWideTile * 2 * D * 2;
-    __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > WAVES * Tile<D>::SLAB ? WIDE_LDS : WAVES * Tile<D>::SLAB];
+    constexpr int STAGES = WIDE ? 1 : 2, NARROW_LDS = WAVES * narrow_slab<D>(STAGES), WIDE_LDS = kStages * kWideTile * 2 * D * 2;
+    __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > NARROW_LDS ? WIDE_LDS : NARROW_LDS];
     __shared__ float sh_m[WAVES][32], sh_l[WAVES][32];
     __shared__ int sh;
     const int lane = threadIdx.x & (kWave - 1);
@@ -924,11 +943,16 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, !WIDE && NARROW_TILES 
     int base = 0;
     Items items = items_at<WIDE, NARROW_TILES>(p, 0, 0, lane);
     unsigned total = __builtin_amdgcn_readlane(items.end, kWave - 1);
-    for (int s = kWave; s < p.items; s += kWave) total = __builtin_amdgcn_readlane(items_at<WIDE, NARROW_TILES>(p, s, total, lane).end, kWave - 1);
+    int number = __popcll(__ballot(items.cost > 0));
+    for (int s = kWave; s < p.items; s += kWave) {
+        const Items more = items_at<WIDE, NARROW_TILES>(p, s, total, lane);
+        total = __builtin_amdgcn_readlane(more.end, kWave - 1);
+        number += __popcll(__ballot(more.cost > 0));
+    }
     if (total == 0) return;
     Pieces pieces;
     pieces.places = (double)total * p.Hkv;
-    pieces.workers = (int)fmin((double)p.workers, fmax(1.0, pieces.places / kMinPiece));
+    pieces.workers = (int)fmin((double)p.workers, fmax((double)number * p.Hkv, pieces.places / kMinPiece));  // (an item's start is no reason to wait for another's)
     if (w >= pieces.workers) return;
     long long at = pieces.start(w);
     const long long end = pieces.start(w + 1);
@@ -957,8 +981,8 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, !WIDE && NARROW_TILES 
         const int each = narrow ? kNarrowCost : kWideCost;
         const long long head = (long long)kvh * total, tile0 = head + item_end - cost + kStartCost;
         auto tile_from = [&](long long place) { return place <= tile0 ? 0 : (int)min((long long)g.tiles, (place - tile0 + each - 1) / each); };
-        g.lo = tile_from(at);
-        g.hi = tile_from(end);
+        g.lo = __builtin_amdgcn_readfirstlane(tile_from(at));
+        g.hi = __builtin_amdgcn_readfirstlane(tile_from(end));
         if (g.lo < g.hi) {
             g.w0 = w;
             g.parts = 1;
@@ -967,10 +991,10 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, !WIDE && NARROW_TILES 
                 g.parts = (g.hi < g.tiles ? pieces.worker(tile0 + (long long)(g.tiles - 1) * each) : w) - g.w0 + 1;
             }
             if constexpr (WIDE) {
-                if (narrow) narrow_segment<D, NARROW_TILES, WAVES>(p, g, w, lds, sh_m, sh_l, &sh);
+                if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, w, lds, sh_m, sh_l, &sh);
                 else wide_segment<D, WAVES>(p, g, w, lds, &sh);
             } else {
-                narrow_segment<D, NARROW_TILES, WAVES>(p, g, w, lds, sh_m, sh_l, &sh);
+                narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, w, lds, sh_m, sh_l, &sh);
             }
         }
         within = item_end;
