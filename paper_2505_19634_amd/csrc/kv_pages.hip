@@ -121,17 +121,20 @@ __device__ __forceinline__ unsigned group_scan(unsigned v, unsigned* sums, unsig
 // found.  Returns how many were.  A wavefront's ballots count its 64 neighbours, LDS holds the counts of a chunk's pieces.
 constexpr int kWalk = 16;                      // pages a thread looks at in a chunk
 constexpr int kChunk = kWalk * kUpkeepThreads;
+__device__ __forceinline__ void load_chunk(const int32_t* refs, int pages, int at, int (&r)[kWalk]) {
+#pragma unroll
+    for (int j = 0; j < kWalk; ++j) {
+        const int i = at + j * kUpkeepThreads + (int)threadIdx.x;
+        r[j] = i < pages ? refs[i] : 0;
+    }
+}
+// r: the first chunk's counts, requested by the caller, who has had other things to wait for.
 template <typename Pick, typename F>
-__device__ __forceinline__ int walk(const int32_t* refs, int pages, int enough, int* counts, Pick pick, F f) {
+__device__ __forceinline__ int walk(const int32_t* refs, int pages, int enough, int* counts, int (&r)[kWalk], Pick pick, F f) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     int found = 0;
     for (int at = 0; at < pages && found < enough; at += kChunk) {
-        int r[kWalk];
-#pragma unroll
-        for (int j = 0; j < kWalk; ++j) {
-            const int i = at + j * kUpkeepThreads + tid;
-            r[j] = i < pages ? refs[i] : 0;
-        }
+        if (at > 0) load_chunk(refs, pages, at, r);
         unsigned long long mask[kWalk];
 #pragma unroll
         for (int j = 0; j < kWalk; ++j) {
@@ -168,7 +171,10 @@ __global__ __launch_bounds__(kUpkeepThreads) void kv_pages_reserve_kernel(const 
     __shared__ unsigned sums[kUpkeepWaves];
     __shared__ int counts[kWalk * kUpkeepWaves];
     __shared__ int bad;
+    __shared__ int list[kUpkeepThreads];
     const int tid = threadIdx.x;
+    int r0[kWalk];
+    load_chunk(p.refs, p.pages, 0, r0);  // whichever pages are free: on their way while the slots are found
     if (tid == 0) bad = 0;
     __syncthreads();
     const int per = (p.B + kUpkeepThreads - 1) / kUpkeepThreads, b0 = tid * per;  // consecutive branches
@@ -214,9 +220,35 @@ __global__ __launch_bounds__(kUpkeepThreads) void kv_pages_reserve_kernel(const 
         x.wanted = none || x.shared;
         return x;
     };
+    if ((int)slots <= kUpkeepThreads) {
+        // a slot a thread, looked at once, and the list in LDS: the usual step of every branch (64 branches x 5 tokens 7.8 -> 5.6 us)
+        Slot x = {};
+        if (tid < (int)slots) x = slot_at(tid);
+        unsigned wanted;
+        const int rank = (int)group_scan(x.wanted, sums, &wanted);
+        const int found = walk(p.refs, p.pages, (int)wanted, counts, r0, [](int, int r) { return r <= 0; },
+                               [&](int i, int before, bool is) {
+                                   if (is && before < (int)wanted) list[before] = i;
+                               });
+        if (tid == 0) *p.count = max(0, (int)wanted - found);
+        if (found < (int)wanted) return;
+        if (x.wanted) {
+            const int page = list[rank];
+            if (x.shared && (long long)x.c << p.shift < p.kv_len[x.b]) {
+                p.out[2 * x.b] = x.entry;
+                p.out[2 * x.b + 1] = page;
+            }
+            p.table[x.b * p.table_stride + x.c] = page;
+            p.refs[page] = 1;
+            if (x.shared) atomicSub(p.refs + x.entry, 1);  // (everybody has looked at the references)
+        }
+        __syncthreads();
+        for (int b = tid; b < p.B; b += kUpkeepThreads) p.kv_len[b] = max(p.kv_len[b], 0) + max(p.arg[b], 0);
+        return;
+    }
     int wanted = 0;
     for (int s0 = 0; s0 < (int)slots; s0 += kUpkeepThreads) wanted += __syncthreads_count(s0 + tid < (int)slots && slot_at(s0 + tid).wanted);
-    const int found = walk(p.refs, p.pages, wanted, counts, [](int, int r) { return r <= 0; },
+    const int found = walk(p.refs, p.pages, wanted, counts, r0, [](int, int r) { return r <= 0; },
                            [&](int i, int before, bool is) {
                                if (is && before < wanted) p.list[before] = i;
                            });
@@ -299,12 +331,16 @@ __global__ __launch_bounds__(256) void kv_pages_fork_kernel(const UpkeepParams p
 __global__ __launch_bounds__(kUpkeepThreads) void kv_pages_compact_kernel(const UpkeepParams p) {
     __shared__ int counts[kWalk * kUpkeepWaves];
     const int tid = threadIdx.x;
-    const int live = walk(p.refs, p.pages, p.pages + 1, counts, [](int, int r) { return r > 0; }, [](int, int, bool) {});
-    const int moves = walk(p.refs, live, live + 1, counts, [](int, int r) { return r <= 0; },
+    int r0[kWalk];
+    load_chunk(p.refs, p.pages, 0, r0);
+    const int live = walk(p.refs, p.pages, p.pages + 1, counts, r0, [](int, int r) { return r > 0; }, [](int, int, bool) {});
+    load_chunk(p.refs, live, 0, r0);
+    const int moves = walk(p.refs, live, live + 1, counts, r0, [](int, int r) { return r <= 0; },
                            [&](int i, int before, bool is) {
                                if (is) p.out[2 * before + 1] = i;
                            });
-    walk(p.refs, p.pages, moves, counts, [&](int i, int r) { return i >= live && r > 0; },
+    load_chunk(p.refs, p.pages, 0, r0);
+    walk(p.refs, p.pages, moves, counts, r0, [&](int i, int r) { return i >= live && r > 0; },
          [&](int i, int before, bool is) {
              if (is) p.out[2 * before] = i;
          });

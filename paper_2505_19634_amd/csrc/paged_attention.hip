@@ -1009,14 +1009,14 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
 
 // ---------------------------------------------------------------------------------------------
 // fp32: fp32 arithmetic throughout, a workgroup per row of a head.  A key row is D / 4 lanes of 16 bytes; a wavefront takes every
-// fourth chunk of 4 * 256 / D keys (no chunk is larger than 16 keys: it lies in one page) and keeps a running state per D / 4 lanes;
+// WAVES-th chunk of 4 * 256 / D keys (no chunk is larger than 16 keys: it lies in one page) and keeps a running state per D / 4 lanes;
 // the states meet at the end.
 // ---------------------------------------------------------------------------------------------
-template <int D>
-__global__ __launch_bounds__(kPgThreads) void paged_f32_kernel(const PagedParams p) {
+template <int D, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedParams p) {
     constexpr int LPK = D / 4, KPL = kWave / LPK, NJ = 4, CHUNK = NJ * KPL;
-    __shared__ __attribute__((aligned(16))) float sh_acc[kPgWaves][D];
-    __shared__ float sh_ml[kPgWaves][2];
+    __shared__ __attribute__((aligned(16))) float sh_acc[WAVES][D];
+    __shared__ float sh_ml[WAVES][2];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     const int grp = lane / LPK, c4 = lane % LPK;
     const int t = blockIdx.x / p.Hq, h = blockIdx.x - t * p.Hq, kvh = quot(h, p.d_g);
@@ -1043,7 +1043,7 @@ __global__ __launch_bounds__(kPgThreads) void paged_f32_kernel(const PagedParams
     const int32_t* row = p.table + b * p.table_stride;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float m = -INFINITY, l = 0.f;
-    for (int j0 = wave * CHUNK; j0 < n; j0 += kPgWaves * CHUNK) {
+    for (int j0 = wave * CHUNK; j0 < n; j0 += WAVES * CHUNK) {
         const int e = __builtin_amdgcn_readfirstlane(row[j0 >> p.shift]);
         if ((unsigned)e >= (unsigned)p.pages) continue;  // no page: nothing to see
         const unsigned char* kp = (const unsigned char*)p.K + e * p.page_p + kvh * p.page_h + c4 * 16;
@@ -1097,10 +1097,10 @@ __global__ __launch_bounds__(kPgThreads) void paged_f32_kernel(const PagedParams
     if (tid < D) {
         float M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kPgWaves; ++w) M = fmaxf(M, sh_ml[w][0]);
+        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, sh_ml[w][0]);
         float lsum = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < kPgWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float wgt = (sh_ml[w][0] == -INFINITY) ? 0.f : expf(sh_ml[w][0] - M);
             lsum += sh_ml[w][1] * wgt;
             o += sh_acc[w][tid] * wgt;
@@ -1215,8 +1215,15 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     const dim3 block(kPgThreads);
     if (d.dtype == LOTTS_F32) {
         const dim3 grid((unsigned)((long long)d.T * d.Hq));
-        if (d.D == 64) LOTTS_LAUNCH(paged_f32_kernel<64>, grid, block, s, p);
-        else LOTTS_LAUNCH(paged_f32_kernel<128>, grid, block, s, p);
+        // A row's keys are a chain of loads: few rows take 16 wavefronts each, so that the chain is short; many fill the chip with 4.  (80 rows of up to
+        // 700 keys 11.6 -> 8.0 us)
+        if ((long long)d.T * d.Hq <= 2 * kNumCU) {
+            if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 16>), grid, dim3(16 * kWave), s, p);
+            else LOTTS_LAUNCH((paged_f32_kernel<128, 16>), grid, dim3(16 * kWave), s, p);
+        } else {
+            if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 4>), grid, block, s, p);
+            else LOTTS_LAUNCH((paged_f32_kernel<128, 4>), grid, block, s, p);
+        }
         return check_launch();
     }
     const dim3 grid((unsigned)pl.workers);
