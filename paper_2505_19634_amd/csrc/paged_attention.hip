@@ -30,8 +30,12 @@ constexpr int kPgGroup = 16;         // keys that lie in one page whatever the p
 constexpr int kNarrowTile = 32;      // keys of a tile of a narrow item: one wavefront's at a time
 constexpr int kWideTile = 64;        // keys of a tile of a wide item: the workgroup's
 constexpr int kWideRows = 256;       // rows of a wide item
-// Places in the sequence of work (below) of a narrow tile, a wide tile, and what starting on an item costs.
-constexpr int kNarrowCost = 2, kWideCost = 5, kStartCost = 6;
+// Places in the sequence of work (below) of a narrow tile, a wide tile, and what starting on an item costs.  Measured where both are in a call: a tile
+// of 32 keys for up to 32 rows 0.27 us at D = 64, 0.6 at 128; one of 64 keys for 256 rows 1.25 and 2.2.  (At 2 : 5, a chunk of 500 beside 31 branches, D = 64,
+// kept some workgroups 34 us and others 68.)
+constexpr int kNarrowCost = 2, kStartCost = 6;
+constexpr int wide_cost(int D) { return D == 64 ? 9 : 7; }
+constexpr int kMaxWideCost = 9;
 constexpr int kMinPiece = 32;        // least places of a worker
 constexpr int kMergeGroup = 8;       // partials that are merged at a time
 
@@ -120,7 +124,7 @@ __device__ __forceinline__ int first_slot(const PagedParams& p, int b) {
     const int first = p.q_start ? min(max(p.q_start[b], 0), p.T) : b * p.R;
     return (int)((long long)first * p.G / kWideRows) + b;
 }
-template <bool WIDE, int NARROW_TILES>
+template <int D, bool WIDE, int NARROW_TILES>
 __device__ __forceinline__ Items items_at(const PagedParams& p, int base, unsigned before, int lane) {
     const int slot = base + lane;
     Items t;
@@ -144,7 +148,7 @@ __device__ __forceinline__ Items items_at(const PagedParams& p, int base, unsign
     const int keys = max(1, br.L - br.n + quot(max(end, 1) - 1, p.d_g) + 1);
     t.b = b; t.first = br.first; t.n = br.n; t.L = br.L;
     t.tiles = narrow ? (keys - 1) / kNarrowTile + 1 : (keys - 1) / kWideTile + 1;
-    t.cost = there ? kStartCost + t.tiles * (narrow ? kNarrowCost : kWideCost) : 0;
+    t.cost = there ? kStartCost + t.tiles * (narrow ? kNarrowCost : wide_cost(D)) : 0;
     t.end = before + wave_incl_scan_u32((unsigned)t.cost);
     return t;
 }
@@ -166,7 +170,9 @@ struct Pieces {
 struct Segment {
     int b, kvh, first, n, L, row0, nrows;
     int lo, hi, tiles;
-    int w0, parts;  // the workers that have tiles of the item: w0 .. w0 + parts - 1
+    int part, parts;              // the item is worked on in `parts` pieces, this is the part-th
+    int slot0, slot1, slot_step;  // where their results lie: slot0, then slot1 + i * slot_step
+    __device__ __forceinline__ int slot(int i) const { return i == 0 ? slot0 : slot1 + i * slot_step; }
 };
 
 // Output quad c4 of row r of a segment: normalised and rounded; the first quad's thread stores the lse.
@@ -181,9 +187,6 @@ __device__ __forceinline__ void store_out(const PagedParams& p, const Segment& g
     *reinterpret_cast<bf16x4*>((unsigned char*)p.O + (long long)(g.first + i) * p.o_t + h * p.o_h + c4 * 8) = v;
     if (p.lse && c4 == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (M + log2f(l)) * 0.69314718055994530942f;
 }
-
-// Slot of worker w's partial of an item: a worker has at most one item that it begins and does not end, and one that it goes on with.
-__device__ __forceinline__ int part_slot(int w, int w0) { return 2 * w + (w == w0 ? 1 : 0); }
 
 // Merges partials [from, from + count) of the segment's item -- every STEP-th of them -- in their order: into the output, or in place of the first.
 template <int D, int WAVES>
@@ -202,7 +205,7 @@ __device__ __forceinline__ void merge_parts(const PagedParams& p, const Segment&
                 ml[j] = make_float2(-INFINITY, 0.f);
                 v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (s0 + j < count) {
-                    const unsigned row = (unsigned)part_slot(g.w0 + from + (s0 + j) * step, g.w0) * p.part_rows + r;
+                    const unsigned row = (unsigned)g.slot(from + (s0 + j) * step) * p.part_rows + r;
                     if (s0 + j == 0) first_at = row;
                     ml[j] = part_load2(rs, p.off_ml + row * 8u);
                     v[j] = part_load4(rs, p.off_o + (row * D + c4 * 4) * 4u);
@@ -235,7 +238,7 @@ __device__ __forceinline__ void merge_parts(const PagedParams& p, const Segment&
 // these have left.  Every wavefront waits for its stores before the count.  A cell starts at the call's tag, which is larger than that
 // of any earlier call, and goes back to zero: a captured launch is replayed with its tag.
 template <int D, int WAVES>
-__device__ __forceinline__ void arrive(const PagedParams& p, const Segment& g, __amdgpu_buffer_rsrc_t rs, int w, int* sh) {
+__device__ __forceinline__ void arrive(const PagedParams& p, const Segment& g, __amdgpu_buffer_rsrc_t rs, int* sh) {
     auto last_of = [&](unsigned long long* cell, int count) {
         __builtin_amdgcn_s_waitcnt(0);  // the wavefront's stores are in memory
         __syncthreads();
@@ -250,15 +253,15 @@ __device__ __forceinline__ void arrive(const PagedParams& p, const Segment& g, _
         __syncthreads();
         return last;
     };
-    const int at = w - g.w0, group = at / kMergeGroup, first = group * kMergeGroup, members = min(kMergeGroup, g.parts - first);
+    const int group = g.part / kMergeGroup, first = group * kMergeGroup, members = min(kMergeGroup, g.parts - first);
     const bool one_group = g.parts <= kMergeGroup;
     if (members > 1) {
-        if (!last_of(p.cells + part_slot(g.w0 + first, g.w0), members)) return;
+        if (!last_of(p.cells + g.slot(first), members)) return;
         merge_parts<D, WAVES>(p, g, rs, first, members, 1, one_group);
     }
     if (one_group) return;
     const int groups = (g.parts - 1) / kMergeGroup + 1;
-    if (!last_of(p.cells + 2 * p.workers + part_slot(g.w0, g.w0), groups)) return;
+    if (!last_of(p.cells + 2 * p.workers + g.slot(0), groups)) return;
     merge_parts<D, WAVES>(p, g, rs, 0, groups, kMergeGroup, true);
 }
 
@@ -383,7 +386,7 @@ __device__ __forceinline__ bf16x8 read_v(unsigned at, int kk, int db) {  // A op
 // A narrow item's part: wavefront w takes tiles lo + w, lo + w + WAVES, ..., through STAGES slabs of its own: with two, the next tile is on its way while
 // one is worked on; with one, the other wavefronts' are.
 template <int D, int TW, int WAVES, int STAGES>
-__device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh) {
+__device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kNarrowTile * ROW, SLAB = narrow_slab<D>(STAGES), LOADS = 4 * X::NLD;  // of a tile
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
@@ -535,13 +538,13 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             if (g.parts == 1) {
                 store_out(p, g, r, c4, o, M, sum);
             } else {
-                const unsigned at = (unsigned)part_slot(w, g.w0) * p.part_rows + r;
+                const unsigned at = (unsigned)g.slot(g.part) * p.part_rows + r;
                 part_store4(rs, p.off_o + (at * D + c4 * 4) * 4u, o);
                 if (c4 == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(M, sum));
             }
         }
     }
-    if (g.parts > 1) arrive<D, WAVES>(p, g, rs, w, sh);
+    if (g.parts > 1) arrive<D, WAVES>(p, g, rs, sh);
     __syncthreads();  // the slabs are free
 }
 
@@ -778,7 +781,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
 
 // The workgroup loads a tile together, 8 keys a wavefront; wavefront w takes row tile w of the item.
 template <int D, int WAVES>
-__device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, int w, unsigned char* lds, int* sh) {
+__device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, unsigned char* lds, int* sh) {
     using X = Tile<D>;
     constexpr int TW = 1, KEYS = kWideTile / WAVES, LOADS = wide_loads<D>();
     static_assert(WAVES * 32 == kWideRows && KEYS * WAVES == kWideTile && KEYS <= kPgGroup && KEYS == LOADS * X::RPI, "a row tile and some keys of a tile for every wavefront");
@@ -897,7 +900,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
         const int r = wave * 32 + ln;
         if (r >= g.nrows) continue;
-        const unsigned at = (unsigned)part_slot(w, g.w0) * p.part_rows + r;
+        const unsigned at = (unsigned)g.slot(g.part) * p.part_rows + r;
         if (g.parts > 1) {
 #pragma unroll
             for (int db = 0; db < X::DB; ++db)
@@ -922,7 +925,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
             }
         if (p.lse && hh == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (m_run[t] * p.scale_log2 + log2f(l)) * 0.69314718055994530942f;
     }
-    if (g.parts > 1) arrive<D, WAVES>(p, g, rs, w, sh);
+    if (g.parts > 1) arrive<D, WAVES>(p, g, rs, sh);
     __syncthreads();
 }
 
@@ -941,11 +944,11 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
     const int per_xcd = p.workers / kNumXCD;  // neighbours in the sequence share an XCD and with it a KV head's keys in its L2
     const int w = (int)(blockIdx.x % kNumXCD) * per_xcd + (int)(blockIdx.x / kNumXCD);
     int base = 0;
-    Items items = items_at<WIDE, NARROW_TILES>(p, 0, 0, lane);
+    Items items = items_at<D, WIDE, NARROW_TILES>(p, 0, 0, lane);
     unsigned total = __builtin_amdgcn_readlane(items.end, kWave - 1);
     int number = __popcll(__ballot(items.cost > 0));
     for (int s = kWave; s < p.items; s += kWave) {
-        const Items more = items_at<WIDE, NARROW_TILES>(p, s, total, lane);
+        const Items more = items_at<D, WIDE, NARROW_TILES>(p, s, total, lane);
         total = __builtin_amdgcn_readlane(more.end, kWave - 1);
         number += __popcll(__ballot(more.cost > 0));
     }
@@ -962,7 +965,7 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
         // the item that has place `within`
         while ((unsigned)__builtin_amdgcn_readlane(items.end, kWave - 1) <= within) {
             base += kWave;
-            items = items_at<WIDE, NARROW_TILES>(p, base, __builtin_amdgcn_readlane(items.end, kWave - 1), lane);
+            items = items_at<D, WIDE, NARROW_TILES>(p, base, __builtin_amdgcn_readlane(items.end, kWave - 1), lane);
         }
         const int i = __builtin_ctzll(__ballot(items.end > within));
         Segment g;
@@ -978,23 +981,28 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
         const bool narrow = !WIDE || rows <= NARROW_TILES * 32;
         if (narrow) g.row0 = 0;
         g.nrows = min(p.part_rows, narrow ? rows : min(kWideRows, rows - g.row0));  // (what max_new allows)
-        const int each = narrow ? kNarrowCost : kWideCost;
+        const int each = narrow ? kNarrowCost : wide_cost(D);
         const long long head = (long long)kvh * total, tile0 = head + item_end - cost + kStartCost;
         auto tile_from = [&](long long place) { return place <= tile0 ? 0 : (int)min((long long)g.tiles, (place - tile0 + each - 1) / each); };
         g.lo = __builtin_amdgcn_readfirstlane(tile_from(at));
         g.hi = __builtin_amdgcn_readfirstlane(tile_from(end));
         if (g.lo < g.hi) {
-            g.w0 = w;
+            int w0 = w;
             g.parts = 1;
             if (g.lo > 0 || g.hi < g.tiles) {
-                g.w0 = g.lo > 0 ? pieces.worker(tile0) : w;
-                g.parts = (g.hi < g.tiles ? pieces.worker(tile0 + (long long)(g.tiles - 1) * each) : w) - g.w0 + 1;
+                w0 = g.lo > 0 ? pieces.worker(tile0) : w;
+                g.parts = (g.hi < g.tiles ? pieces.worker(tile0 + (long long)(g.tiles - 1) * each) : w) - w0 + 1;
             }
+            g.part = w - w0;
+            // a worker has at most one item that it begins and does not end, and one that it goes on with
+            g.slot0 = 2 * w0 + 1;
+            g.slot1 = 2 * w0;
+            g.slot_step = 2;
             if constexpr (WIDE) {
-                if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, w, lds, sh_m, sh_l, &sh);
-                else wide_segment<D, WAVES>(p, g, w, lds, &sh);
+                if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
+                else wide_segment<D, WAVES>(p, g, lds, &sh);
             } else {
-                narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, w, lds, sh_m, sh_l, &sh);
+                narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
             }
         }
         within = item_end;
@@ -1002,7 +1010,7 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
         if (within >= total) {
             ++kvh;
             within = 0;
-            if (base > 0) items = items_at<WIDE, NARROW_TILES>(p, base = 0, 0, lane);
+            if (base > 0) items = items_at<D, WIDE, NARROW_TILES>(p, base = 0, 0, lane);
         }
     }
 }
@@ -1144,7 +1152,7 @@ static int paged_desc(const lotts_paged_desc* in, bool uniform, lotts_paged_desc
     if (d->page_stride_t * es > (1LL << 26)) return LOTTS_ERR_SHAPE;  // 16 keys of a page: 32-bit offsets
     // the sequence of work of a KV head in 32 bits (were every branch as long as the table allows)
     const long long G = d->Hq / d->Hkv, slots = (long long)d->T * G / kWideRows + d->B;
-    if (((long long)d->columns << *shift) / kNarrowTile * kNarrowCost + kWideCost + kStartCost > 0x7fffffffLL / slots) return LOTTS_ERR_SHAPE;
+    if (((long long)d->columns << *shift) / kNarrowTile * kMaxWideCost + kMaxWideCost + kStartCost > 0x7fffffffLL / slots) return LOTTS_ERR_SHAPE;
     if ((long long)d->T * d->Hq >= (1LL << 24)) return LOTTS_ERR_SHAPE;  // a grid holds fewer than 2^24 workgroups of 256 threads
     return LOTTS_OK;
 }
