@@ -36,7 +36,8 @@ constexpr int kWideRows = 256;       // rows of a wide item
 constexpr int kNarrowCost = 2, kStartCost = 6;
 constexpr int wide_cost(int D) { return D == 64 ? 9 : 7; }
 constexpr int kMaxWideCost = 9;
-constexpr int kMinPiece = 32;        // least places of a worker
+constexpr int kMinPiece = 32;        // places of a worker below which there are no more workers than items
+constexpr int kApartPlaces = 280;    // places of a worker below which items are cut one by one
 constexpr int kMergeGroup = 8;       // partials that are merged at a time
 
 struct PagedParams {
@@ -953,20 +954,53 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
         number += __popcll(__ballot(more.cost > 0));
     }
     if (total == 0) return;
+    // Every piece has at least one tile of an item that it lies in: whoever counts an item's parts counts on that.
+    constexpr int LEAST = WIDE ? kMaxWideCost + 1 : kNarrowCost + 2;
     Pieces pieces;
     pieces.places = (double)total * p.Hkv;
-    pieces.workers = (int)fmin((double)p.workers, fmax((double)number * p.Hkv, pieces.places / kMinPiece));  // (an item's start is no reason to wait for another's)
-    if (w >= pieces.workers) return;
-    long long at = pieces.start(w);
-    const long long end = pieces.start(w + 1);
-    int kvh = (int)(at / total);
-    unsigned within = (unsigned)(at - (long long)kvh * total);
-    while (at < end) {
-        // the item that has place `within`
-        while ((unsigned)__builtin_amdgcn_readlane(items.end, kWave - 1) <= within) {
-            base += kWave;
-            items = items_at<D, WIDE, NARROW_TILES>(p, base, __builtin_amdgcn_readlane(items.end, kWave - 1), lane);
+    const double all = (double)number * p.Hkv;  // items
+    pieces.workers = (int)fmax(1.0, fmin(fmin((double)p.workers, pieces.places / LEAST), fmax(all, pieces.places / kMinPiece)));  // (an item's start is no reason to wait for another's)
+    // Short calls with wide items are cut item by item: a cut costs as much as 2 to 4 tiles (256 rows of partial outputs out and in), and a piece of the sequence
+    // mostly ends one item and begins another, with a cut on either side.  Each worker gets one part of one item, of about `size` places.
+    bool apart = false;
+    double size = 0.0;
+    unsigned parts_total = 0;
+    auto parts_of = [&](Items& t, unsigned before) {
+        t.cost = t.cost > 0 ? max(1, (int)ceil((t.cost - kStartCost) / size)) : 0;
+        t.end = before + wave_incl_scan_u32((unsigned)t.cost);
+    };
+    if (WIDE && all <= 0.75 * p.workers && pieces.places < kApartPlaces * (double)p.workers) {
+        size = fmax(1.0, (pieces.places - all * kStartCost) / (p.workers - 0.6 * all));
+        for (int s = 0; s < p.items; s += kWave) {
+            Items more = items;
+            if (s > 0) more = items_at<D, WIDE, NARROW_TILES>(p, s, 0, lane);
+            parts_of(more, parts_total);
+            parts_total = __builtin_amdgcn_readlane(more.end, kWave - 1);
         }
+        apart = parts_total * (double)p.Hkv <= 2.0 * p.workers;  // as many slots for partials as there are
+    }
+    long long at, end;
+    if (apart) {
+        parts_of(items, 0);
+        total = parts_total;
+        at = w;
+        end = (long long)total * p.Hkv;
+    } else {
+        if (w >= pieces.workers) return;
+        at = pieces.start(w);
+        end = pieces.start(w + 1);
+    }
+    while (at < end) {
+        const int kvh = __builtin_amdgcn_readfirstlane((int)(at / total));
+        const long long head = (long long)kvh * total;
+        const unsigned within = __builtin_amdgcn_readfirstlane((unsigned)(at - head));
+        auto load = [&](int from, unsigned before) {
+            items = items_at<D, WIDE, NARROW_TILES>(p, base = from, before, lane);
+            if (apart) parts_of(items, before);
+        };
+        // the item that has place `within`
+        if (base > 0 && (unsigned)(__builtin_amdgcn_readlane(items.end, 0) - __builtin_amdgcn_readlane(items.cost, 0)) > within) load(0, 0);
+        while ((unsigned)__builtin_amdgcn_readlane(items.end, kWave - 1) <= within) load(base + kWave, __builtin_amdgcn_readlane(items.end, kWave - 1));
         const int i = __builtin_ctzll(__ballot(items.end > within));
         Segment g;
         g.b = __builtin_amdgcn_readlane(items.b, i);
@@ -981,15 +1015,23 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
         const bool narrow = !WIDE || rows <= NARROW_TILES * 32;
         if (narrow) g.row0 = 0;
         g.nrows = min(p.part_rows, narrow ? rows : min(kWideRows, rows - g.row0));  // (what max_new allows)
-        const int each = narrow ? kNarrowCost : wide_cost(D);
-        const long long head = (long long)kvh * total, tile0 = head + item_end - cost + kStartCost;
-        auto tile_from = [&](long long place) { return place <= tile0 ? 0 : (int)min((long long)g.tiles, (place - tile0 + each - 1) / each); };
-        g.lo = __builtin_amdgcn_readfirstlane(tile_from(at));
-        g.hi = __builtin_amdgcn_readfirstlane(tile_from(end));
-        if (g.lo < g.hi) {
+        if (apart) {
+            g.part = (int)(within - (item_end - cost));
+            g.parts = min(cost, g.tiles);
+            g.lo = (int)((long long)g.tiles * g.part / g.parts);
+            g.hi = g.part < g.parts ? (int)((long long)g.tiles * (g.part + 1) / g.parts) : g.lo;
+            g.slot0 = g.slot1 = (int)(head + item_end - cost);
+            g.slot_step = 1;
+            at += p.workers;
+        } else {
+            const int each = narrow ? kNarrowCost : wide_cost(D);
+            const long long tile0 = head + item_end - cost + kStartCost;
+            auto tile_from = [&](long long place) { return place <= tile0 ? 0 : (int)min((long long)g.tiles, (place - tile0 + each - 1) / each); };
+            g.lo = tile_from(at);
+            g.hi = tile_from(end);
             int w0 = w;
             g.parts = 1;
-            if (g.lo > 0 || g.hi < g.tiles) {
+            if (g.lo < g.hi && (g.lo > 0 || g.hi < g.tiles)) {
                 w0 = g.lo > 0 ? pieces.worker(tile0) : w;
                 g.parts = (g.hi < g.tiles ? pieces.worker(tile0 + (long long)(g.tiles - 1) * each) : w) - w0 + 1;
             }
@@ -998,19 +1040,16 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
             g.slot0 = 2 * w0 + 1;
             g.slot1 = 2 * w0;
             g.slot_step = 2;
-            if constexpr (WIDE) {
-                if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
-                else wide_segment<D, WAVES>(p, g, lds, &sh);
-            } else {
-                narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
-            }
+            at = head + item_end;
         }
-        within = item_end;
-        at = head + within;
-        if (within >= total) {
-            ++kvh;
-            within = 0;
-            if (base > 0) items = items_at<D, WIDE, NARROW_TILES>(p, base = 0, 0, lane);
+        g.lo = __builtin_amdgcn_readfirstlane(g.lo);
+        g.hi = __builtin_amdgcn_readfirstlane(g.hi);
+        if (g.lo >= g.hi) continue;
+        if constexpr (WIDE) {
+            if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
+            else wide_segment<D, WAVES>(p, g, lds, &sh);
+        } else {
+            narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
         }
     }
 }

@@ -69,6 +69,27 @@ def test_many_branches(lotts, B, dtype):
     check(c, *attend(lotts, c, max_new=3))
 
 
+@pytest.mark.parametrize("tiny", [3, 100, 400])
+@pytest.mark.parametrize("chunk,L", [(90, 90), (150, 1000), (700, 3100)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_chunk_beside_tiny_branches(lotts, tiny, chunk, L, D):
+    """The work's equal pieces may be as small as a tile of the chunk is long: every one of them has a part of it."""
+    print("paged attention", tiny, chunk, L, D, flush=True)
+    new = [1 + b % 2 for b in range(tiny // 2)] + [chunk] + [1] * (tiny - tiny // 2)
+    length = [n + b % 3 for b, n in enumerate(new)]
+    length[tiny // 2] = L
+    c = Cache(new, length, 4, 2 if tiny < 100 else 1, D, 16, seed=tiny + chunk)
+    check(c, *attend(lotts, c, max_new=chunk))
+
+
+@pytest.mark.parametrize("n,L,Hq,Hkv", [(300, 300, 16, 2), (1030, 1500, 8, 8), (513, 4000, 5, 1), (2039, 2039, 16, 2), (260, 9000, 2, 1)])
+def test_prompts(lotts, n, L, Hq, Hkv):
+    """Items that are cut one by one, a few parts each."""
+    print("paged attention", n, L, Hq, Hkv, flush=True)
+    c = Cache([n], [L], Hq, Hkv, 128 if Hq != 5 else 64, 64, seed=n)
+    check(c, *attend(lotts, c, max_new=n))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("page", [16, 32, 64])
 def test_missing_pages(lotts, page, dtype):
