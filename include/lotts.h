@@ -328,12 +328,15 @@ size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc *desc);
  *                 a branch without new tokens.  NULL: every branch has T / B of them (T % B == 0, max_new = T / B)
  *   lse           [T][Hq] fp32, out, may be NULL: natural-log sum of exp of the scaled scores
  *   workspace     >= verify_attention_paged_workspace_bytes(desc), 16-byte aligned; as for verify_attention: zero-filled once before its
- *                 first use, then this entry point's own, shared by calls that are ordered on one stream
+ *                 first use, then this entry point's own, shared by calls that are ordered on one stream (a captured one's replays
+ *                 included: two graphs that may run at the same time have a buffer each)
  * kv_len, q_start and the table are device data and are not checked on the host: the kernels keep whatever they address inside the buffers
  * that the descriptor describes, but the rows of a branch whose data break the contract are then unspecified.
  * What a cache row holds behind the branch's last token does not matter, NaN included.  (A row's weight for a later token of the same
  * chunk is exactly 0; in bf16 an infinity or NaN among the chunk's own V rows reaches the rows in front of it all the same.)
  * bf16 inputs are multiplied on the matrix cores with fp32 accumulation; fp32 inputs are computed in fp32 throughout.
+ * Every call with the same data gives the same bits.  In bf16 the lengths of all branches of a call decide where a branch's keys are cut: other
+ * lengths beside it may change its last bits.  Scores are taken to be below 2^29 in magnitude once scaled.
  */
 int verify_attention_paged(const lotts_paged_desc *desc, const void *Q, const void *Kpages, const void *Vpages, const int32_t *page_table,
                            const int32_t *kv_len, const int32_t *q_start, void *O, float *lse, void *workspace, size_t workspace_bytes,

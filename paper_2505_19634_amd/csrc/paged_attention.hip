@@ -24,8 +24,6 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPgMaxBranches = 4096;
 constexpr int kPgMaxPages = 1 << 24;
-constexpr int kPgThreads = 256;
-constexpr int kPgWaves = kPgThreads / kWave;
 constexpr int kPgGroup = 16;         // keys that lie in one page whatever the page size
 constexpr int kNarrowTile = 32;      // keys of a tile of a narrow item: one wavefront's at a time
 constexpr int kWideTile = 64;        // keys of a tile of a wide item: the workgroup's
@@ -266,8 +264,7 @@ __device__ __forceinline__ void arrive(const PagedParams& p, const Segment& g, _
     merge_parts<D, WAVES>(p, g, rs, 0, groups, kMergeGroup, true);
 }
 
-// What a wavefront knows of the pages of the tiles ahead: lane i has the entries of the i-th tile from `base` on, STEP tiles apart.  One load
-// for 64 tiles, so that no tile waits for its entry.
+// A branch's entry for a key.  (Both kinds of item look up 64 tiles' at a time, a lane each, so that no tile waits for its entry.)
 __device__ __forceinline__ int page_entry(const PagedParams& p, const int32_t* row, int key) { return row[min(key >> p.shift, p.columns - 1)]; }
 
 // 16 keys of a page: the buffer ends behind the last one that there is, so that keys behind it, and those without a page, read as zeros.
@@ -556,80 +553,76 @@ __device__ constexpr int wide_loads() {
     return D == 128 ? 2 : 1;
 }
 
-// The products of a wide item are written as instructions, so that every operand lies where it should: outputs and Q in accumulation registers,
-// scores where the vector units reach them.  (Left to choose, the compiler put the scores into accumulation registers too, Q into scratch memory
-// and the waits for that into the loop.)  It does not know how long these take: what reads a result on the vector units is kept behind
-// two later products, or behind mfma_done().
+// The products of a wide item are written as instructions, on vector registers, so that a slot of the loop below holds what it was given.  (Left to choose, the
+// compiler put the scores into accumulation registers, Q into scratch memory and the waits for that into the loop.)  It does not know how long
+// these take: what reads a result on the vector units is kept behind two later products, or behind mfma_done().
 __device__ __forceinline__ void mfma_first(f32x16& d, const bf16x8& a, const bf16x8& b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
 }
-__device__ __forceinline__ void mfma_scores(f32x16& d, const bf16x8& a, const bf16x8& b) {
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
-}
-__device__ __forceinline__ void mfma_output(f32x16& d, const bf16x8& a, const bf16x8& b) {
+__device__ __forceinline__ void mfma_onto(f32x16& d, const bf16x8& a, const bf16x8& b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_done() { asm volatile("s_nop 15\n\ts_nop 15"); }
 
-// The loop over a wide item's tiles for a wavefront with N row tiles.  arrive(): the next tile is in LDS for everybody; request(j, v, i): load i of the
+// The loop over a wide item's tiles for a wavefront with a row tile.  arrive(): the next tile is in LDS for everybody; request(j, v, i): load i of the
 // wavefront's part of tile j's K or V.  In a step 32 keys are weighed and multiplied with V while the next 32 are multiplied with Q and their maximum
-// is found.  A wavefront has its SIMD to itself and issues in order: a product takes its 32 cycles beside whatever comes behind it, but a
-// vector instruction that needs the one before it waits 8 cycles (independent ones take 4 to 5, an exponential 9).  So the step is
+// is found.  Two wavefronts share a SIMD, each issues in order: a product takes 32 cycles of the matrix unit beside whatever comes behind it, but a
+// vector instruction that needs the one before it waits 8 cycles (independent ones take 4 to 8 by their length, an exponential 9).  So the step is
 // written down as slots of one product each, and a pair of weights goes through three of them -- scaled, exponential, rounded and summed -- so
-// that nothing in a slot depends on anything else in it; scheduling barriers keep the slots apart.  (With a pair's whole chain in one slot a step of 2 row
-// tiles took 2300 cycles, the products alone take 1024.)
-template <int D, int N, typename Arrive, typename Request>
-__device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[N][Tile<D>::KS], const int (&lim)[N],
-                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[N][Tile<D>::DB], float (&m)[N], float (&l)[N], Arrive arrive, Request request) {
+// that nothing in a slot depends on anything else in it; scheduling barriers keep the slots apart.  Loads go out a few a step: all of a tile's at
+// once held the wavefronts 1000 to 1600 cycles a tile.  (4 wavefronts of two row tiles, a SIMD each: a prompt of 2039 tokens,
+// 16 / 2 heads, 81 us against 62 with 8; 2 chunks of 2048 alike.)
+template <int D, typename Arrive, typename Request>
+__device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[Tile<D>::KS], int lim,
+                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[Tile<D>::DB], float& m, float& l, Arrive arrive, Request request) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
-    constexpr int QG = X::KS, VG = 2 * X::DB;   // groups of products with 32 keys of K and of V, N products each
-    constexpr int QS = QG * N, VS = VG * N;     // slots
+    constexpr int QS = X::KS, VS = 2 * X::DB;   // slots: products of 32 keys with K and with V
     constexpr int LOADS = wide_loads<D>(), EARLY = LOADS / 2;  // of a wavefront and operand; those beside products with K
-    constexpr int AHEAD = 3;                    // groups between a read from LDS and its use
-    constexpr int PAIRS = 8 * N;                // pairs of weights: the first half goes into the first half of the products with V
-    constexpr int SPAN = (QG + X::DB) * N - (D == 64 ? 3 : 2);  // slots over which they begin: done two slots before their product
+    constexpr int AHEAD = 3;                    // slots between a read from LDS and its use
+    constexpr int PAIRS = 8;                    // pairs of weights: the first half goes into the first half of the products with V
+    constexpr int SPAN = QS + X::DB - (D == 64 ? 3 : 2);  // slots over which they begin: done two slots before their product
     constexpr int LOOK = QS + 2, LOOKS = VS - 3;  // slots that look at the next scores: two products behind the last one that makes them, up to the last but one
-    float negm[N], mx[N], l2[N];  // l2: the sums of every second weight
-    f32x16 sa[N], sb[N];  // scores as products leave them, in turns: of the keys that are weighed, of the next ones
-    bf16x8 pf[N][2];
-    const float scale = p.scale_log2, rescale = kRescale / scale;
+    float negm = 0.f, mx = -INFINITY, l2 = 0.f;  // l2: the sums of every second weight
+    f32x16 sa, sb;  // scores as products leave them, in turns: of the keys that are weighed, of the next ones
+    bf16x8 pf[2];
+    const float scale = p.scale_log2, rescale = fminf(kRescale / scale, 3.0e38f);  // (finite however small the scale: the first maximum always counts)
     auto read_k = [&](unsigned st, int i) { return lotts::read_k<D>(st + kat, i); };
     auto read_v = [&](unsigned st, int i) { return lotts::read_v<D>(st + vat, i / X::DB, i % X::DB); };
     // (Every result is pinned where it is computed: the compiler would move it down to its use, behind the mask's branch.)
-    auto scale_pair = [&](f32x16 (&c)[N], int q) {
-        const int t = q % N, x = q / N * 2;
-        float u = __builtin_fmaf(c[t][x], scale, negm[t]), v = __builtin_fmaf(c[t][x + 1], scale, negm[t]);
+    auto scale_pair = [&](f32x16& c, int q) {
+        const int x = q * 2;
+        float u = __builtin_fmaf(c[x], scale, negm), v = __builtin_fmaf(c[x + 1], scale, negm);
         asm volatile("" : "+v"(u), "+v"(v));
-        c[t][x] = u;
-        c[t][x + 1] = v;
+        c[x] = u;
+        c[x + 1] = v;
     };
-    auto weigh_pair = [&](f32x16 (&c)[N], int q) {
-        const int t = q % N, x = q / N * 2;
-        float u = __builtin_amdgcn_exp2f(c[t][x]), v = __builtin_amdgcn_exp2f(c[t][x + 1]);
+    auto weigh_pair = [&](f32x16& c, int q) {
+        const int x = q * 2;
+        float u = __builtin_amdgcn_exp2f(c[x]), v = __builtin_amdgcn_exp2f(c[x + 1]);
         asm volatile("" : "+v"(u), "+v"(v));
-        c[t][x] = u;
-        c[t][x + 1] = v;
+        c[x] = u;
+        c[x + 1] = v;
     };
-    auto sum_pair = [&](f32x16 (&c)[N], int q) {
-        const int t = q % N, x = q / N * 2;
+    auto sum_pair = [&](f32x16& c, int q) {
+        const int x = q * 2;
         // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
-        const f32x2 pair = {c[t][x], c[t][x + 1]};
+        const f32x2 pair = {c[x], c[x + 1]};
         unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, bf16x2));
-        l[t] += c[t][x];
-        l2[t] += c[t][x + 1];
-        asm volatile("" : "+v"(l[t]), "+v"(l2[t]), "+v"(u));
-        u32x4 all = __builtin_bit_cast(u32x4, pf[t][x >> 3]);
+        l += c[x];
+        l2 += c[x + 1];
+        asm volatile("" : "+v"(l), "+v"(l2), "+v"(u));
+        u32x4 all = __builtin_bit_cast(u32x4, pf[x >> 3]);
         all[(x & 7) >> 1] = u;
-        pf[t][x >> 3] = __builtin_bit_cast(bf16x8, all);
+        pf[x >> 3] = __builtin_bit_cast(bf16x8, all);
     };
-    auto look = [&](const f32x16 (&n)[N], int r) {  // a pair of the next scores
-        const int t = r % N, x = r / N * 2;
-        mx[t] = fmaxf(fmaxf(mx[t], n[t][x]), n[t][x + 1]);
-        asm volatile("" : "+v"(mx[t]));
+    auto look = [&](const f32x16& n, int r) {  // a pair of the next scores
+        const int x = r * 2;
+        mx = fmaxf(fmaxf(mx, n[x]), n[x + 1]);
+        asm volatile("" : "+v"(mx));
     };
     // what goes beside the product of slot i
-    auto beside = [&](f32x16 (&c)[N], const f32x16 (&n)[N], int i) {
+    auto beside = [&](f32x16& c, const f32x16& n, int i) {
 #pragma unroll
         for (int q = 0; q < PAIRS; ++q) {
             if (q * SPAN / PAIRS + 2 == i) sum_pair(c, q);
@@ -642,73 +635,61 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
                 if (LOOK + r * LOOKS / PAIRS == i) look(n, r);
         }
     };
-    auto mask = [&](f32x16 (&n)[N], int kb, int have) {
+    auto mask = [&](f32x16& n, int kb, int have) {
         if ((have & 3) == 3 && kb + 32 <= first_lim) return;
         mfma_done();
         const int hh = (threadIdx.x & 32) >> 5;
+        const int vis = lim - kb - hh * 4;
 #pragma unroll
-        for (int t = 0; t < N; ++t) {
-            const int vis = lim[t] - kb - hh * 4;
-#pragma unroll
-            for (int x = 0; x < 16; ++x) n[t][x] = (x >> 2) * 8 + (x & 3) < vis && (have >> (x >> 3) & 1) ? n[t][x] : -INFINITY;
-        }
+        for (int x = 0; x < 16; ++x) n[x] = (x >> 2) * 8 + (x & 3) < vis && (have >> (x >> 3) & 1) ? n[x] : -INFINITY;
     };
-    bool rise[N];
-    auto find_rise = [&](int t) {
-        mx[t] = max_halves(mx[t]);
-        rise[t] = mx[t] > m[t] + rescale;
+    bool rise = false;
+    auto find_rise = [&] {
+        mx = max_halves(mx);
+        rise = mx > m + rescale;
     };
     auto settle = [&] {  // o and l follow where the maximum has risen much
-        bool any = rise[0];
-        if (N > 1) any = any || rise[N - 1];
-        if (__builtin_amdgcn_ballot_w64(any) != 0) {
+        if (__builtin_amdgcn_ballot_w64(rise) != 0) {
             mfma_done();
+            const float m_new = rise ? mx : m, base = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f((m - base) * scale);
+            m = m_new;
+            negm = -base * scale;
+            l *= alpha;
+            l2 *= alpha;
 #pragma unroll
-            for (int t = 0; t < N; ++t) {
-                const float m_new = rise[t] ? mx[t] : m[t], base = m_new == -INFINITY ? 0.f : m_new;
-                const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * scale);
-                m[t] = m_new;
-                negm[t] = -base * scale;
-                l[t] *= alpha;
-                l2[t] *= alpha;
+            for (int db = 0; db < X::DB; ++db)
 #pragma unroll
-                for (int db = 0; db < X::DB; ++db)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[t][db][i] *= alpha;
-            }
+                for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
         }
-#pragma unroll
-        for (int t = 0; t < N; ++t) mx[t] = -INFINITY;
+        mx = -INFINITY;
     };
-    auto multiply_k = [&](f32x16 (&n)[N], int t, int i, const bf16x8& k) {
-        if (i == 0) mfma_first(n[t], k, qf[t][i]);
-        else mfma_scores(n[t], k, qf[t][i]);
+    auto multiply_k = [&](f32x16& n, int i, const bf16x8& k) {
+        if (i == 0) mfma_first(n, k, qf[i]);
+        else mfma_onto(n, k, qf[i]);
     };
-    auto multiply_v = [&](int t, int i, const bf16x8& v) { mfma_output(o[t][i % X::DB], v, pf[t][i / X::DB]); };
+    auto multiply_v = [&](int i, const bf16x8& v) { mfma_onto(o[i % X::DB], v, pf[i / X::DB]); };
     bf16x8 k0[AHEAD];  // the first pieces of K of the step ahead
     int have;
     unsigned st = lo % kStages * STAGE;
     // Step j: the scores in c, of the keys at st, are weighed and multiplied with V, those of the j-th 32 keys of all go into n.
-    auto step = [&](f32x16 (&c)[N], f32x16 (&n)[N], int j) {
+    auto step = [&](f32x16& c, f32x16& n, int j) {
         const unsigned before = st;
         st = (j >> 1) % kStages * STAGE + (j & 1) * 32 * ROW;
         have >>= 2;
-        bf16x8 f[QG + VG];
+        bf16x8 f[QS + VS];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) f[i] = k0[i];
 #pragma unroll
-        for (int i = 0; i < QG; ++i) {
+        for (int i = 0; i < QS; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            f[i + AHEAD] = i + AHEAD < QG ? read_k(st, i + AHEAD) : read_v(before, i + AHEAD - QG);
-#pragma unroll
-            for (int t = 0; t < N; ++t) {
-                multiply_k(n, t, i, f[i]);
-                beside(c, n, i * N + t);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            f[i + AHEAD] = i + AHEAD < QS ? read_k(st, i + AHEAD) : read_v(before, i + AHEAD - QS);
+            multiply_k(n, i, f[i]);
+            beside(c, n, i);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int r = 0; r < EARLY; ++r)
-                if (i == (2 * r + 1) * QG / (2 * (EARLY > 0 ? EARLY : 1))) request((j >> 1) + 2, j & 1, r);
+                if (i == (2 * r + 1) * QS / (2 * (EARLY > 0 ? EARLY : 1))) request((j >> 1) + 2, j & 1, r);
         }
         if (D == 64) asm volatile("s_nop 1");  // (the first half's last weights were rounded in the slot before)
         mask(n, j * 32, have);
@@ -716,25 +697,22 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         if ((j & 1) != 0 && j + 1 < 2 * hi) have = arrive(false) << 2;
         const unsigned after = ((j + 1) >> 1) % kStages * STAGE + ((j + 1) & 1) * 32 * ROW;
 #pragma unroll
-        for (int i = 0; i < VG; ++i) {
+        for (int i = 0; i < VS; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            if (i + AHEAD < VG) f[QG + i + AHEAD] = read_v(before, i + AHEAD);
-            else k0[i + AHEAD - VG] = read_k(after, i + AHEAD - VG);
-#pragma unroll
-            for (int t = 0; t < N; ++t) {
-                multiply_v(t, i, f[QG + i]);
-                beside(c, n, QS + i * N + t);
-                if (i == VG - 1) find_rise(t);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            if (i + AHEAD < VS) f[QS + i + AHEAD] = read_v(before, i + AHEAD);
+            else k0[i + AHEAD - VS] = read_k(after, i + AHEAD - VS);
+            multiply_v(i, f[QS + i]);
+            beside(c, n, QS + i);
+            if (i == VS - 1) find_rise();
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int r = EARLY; r < LOADS; ++r)
-                if (i == (2 * (r - EARLY) + 1) * VG / (2 * (LOADS - EARLY))) request((j >> 1) + 2, j & 1, r);
+                if (i == (2 * (r - EARLY) + 1) * VS / (2 * (LOADS - EARLY))) request((j >> 1) + 2, j & 1, r);
         }
         settle();
     };
     // the last scores: nothing is left to multiply with Q
-    auto finish = [&](f32x16 (&c)[N]) {
+    auto finish = [&](f32x16& c) {
 #pragma unroll
         for (int q = 0; q < PAIRS; ++q) scale_pair(c, q);
 #pragma unroll
@@ -743,30 +721,25 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         for (int q = 0; q < PAIRS; ++q) sum_pair(c, q);
         asm volatile("s_nop 1");
 #pragma unroll
-        for (int i = 0; i < VG; ++i) {
+        for (int i = 0; i < VS; ++i) {
             const bf16x8 v = read_v(st, i);
-#pragma unroll
-            for (int t = 0; t < N; ++t) multiply_v(t, i, v);
+            multiply_v(i, v);
         }
         mfma_done();
     };
-#pragma unroll
-    for (int t = 0; t < N; ++t) negm[t] = 0.f, mx[t] = -INFINITY, l2[t] = 0.f;
     have = arrive(true);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) request(lo + 2, 0, i);
 #pragma unroll
-    for (int i = 0; i < QG; ++i) {
+    for (int i = 0; i < QS; ++i) {
         const bf16x8 k = read_k(st, i);
-#pragma unroll
-        for (int t = 0; t < N; ++t) multiply_k(sa, t, i, k);
+        multiply_k(sa, i, k);
     }
     mfma_done();
     mask(sa, lo * kWideTile, have);
 #pragma unroll
     for (int r = 0; r < PAIRS; ++r) look(sa, r);
-#pragma unroll
-    for (int t = 0; t < N; ++t) find_rise(t);
+    find_rise();
     settle();
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) k0[i] = read_k(st + 32 * ROW, i);
@@ -776,15 +749,14 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     }
     step(sa, sb, 2 * hi - 1);
     finish(sb);
-#pragma unroll
-    for (int t = 0; t < N; ++t) l[t] += l2[t];
+    l += l2;
 }
 
 // The workgroup loads a tile together, 8 keys a wavefront; wavefront w takes row tile w of the item.
 template <int D, int WAVES>
 __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, unsigned char* lds, int* sh) {
     using X = Tile<D>;
-    constexpr int TW = 1, KEYS = kWideTile / WAVES, LOADS = wide_loads<D>();
+    constexpr int KEYS = kWideTile / WAVES, LOADS = wide_loads<D>();
     static_assert(WAVES * 32 == kWideRows && KEYS * WAVES == kWideTile && KEYS <= kPgGroup && KEYS == LOADS * X::RPI, "a row tile and some keys of a tile for every wavefront");
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;  // bytes
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
@@ -855,31 +827,20 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         have_0 = have_1;
         return have;
     };
-    bf16x8 qf[TW][X::KS];
-    int lim[TW];
+    const int q_row = min(g.row0 + wave * 32 + ln, g.row0 + g.nrows - 1), q_token = quot(q_row, p.d_g), lim = before + q_token + 1;
+    const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + q_token) * p.q_t + (g.kvh * p.G + q_row - q_token * p.G) * p.q_h;
+    bf16x8 qf[X::KS];
 #pragma unroll
-    for (int t = 0; t < TW; ++t) {
-        const int r = min(g.row0 + wave * 32 + ln, g.row0 + g.nrows - 1), i = quot(r, p.d_g);
-        lim[t] = before + i + 1;
-        const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
-#pragma unroll
-        for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
-    }
+    for (int s = 0; s < X::KS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
     const unsigned kat = lds_address(lds) + lane_of_k<D>(lane), vat = lds_address(lds) + HALF + lane_of_v<D>(lane);
-    f32x16 oacc[TW][X::DB];
-    float m_run[TW], l_run[TW];
+    f32x16 oacc[X::DB];
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-    for (int t = 0; t < TW; ++t) {
-        m_run[t] = -INFINITY;
-        l_run[t] = 0.f;
+    for (int db = 0; db < X::DB; ++db)
 #pragma unroll
-        for (int db = 0; db < X::DB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
-    }
-    const int row_tiles = __builtin_amdgcn_readfirstlane((g.nrows + 31) / 32 - wave);  // from this wavefront's first on
-    if (row_tiles > 0) {
-        wide_rows<D, TW>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
+        for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
+    if (wave * 32 < g.nrows) {
+        wide_rows<D>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
     } else {  // no rows: the loads and the meetings alone, in the same order
         arrive_tile(true);
 #pragma unroll
@@ -896,22 +857,17 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
-#pragma unroll
-    for (int t = 0; t < TW; ++t) {
-        const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
-        const int r = wave * 32 + ln;
-        if (r >= g.nrows) continue;
+    const float l = l_run + shfl_xor_f(l_run, 32);
+    const int r = wave * 32 + ln;
+    if (r < g.nrows && g.parts > 1) {
         const unsigned at = (unsigned)g.slot(g.part) * p.part_rows + r;
-        if (g.parts > 1) {
 #pragma unroll
-            for (int db = 0; db < X::DB; ++db)
+        for (int db = 0; db < X::DB; ++db)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    part_store4(rs, p.off_o + (at * D + db * 32 + q * 8 + hh * 4) * 4u,
-                                make_float4(oacc[t][db][q * 4], oacc[t][db][q * 4 + 1], oacc[t][db][q * 4 + 2], oacc[t][db][q * 4 + 3]));
-            if (hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run[t] * p.scale_log2, l));
-            continue;
-        }
+            for (int q = 0; q < 4; ++q)
+                part_store4(rs, p.off_o + (at * D + db * 32 + q * 8 + hh * 4) * 4u, make_float4(oacc[db][q * 4], oacc[db][q * 4 + 1], oacc[db][q * 4 + 2], oacc[db][q * 4 + 3]));
+        if (hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run * p.scale_log2, l));
+    } else if (r < g.nrows) {
         const int i = quot(g.row0 + r, p.d_g), h = g.kvh * p.G + g.row0 + r - i * p.G;
         const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing is 0
         unsigned char* op = (unsigned char*)p.O + (long long)(g.first + i) * p.o_t + h * p.o_h;
@@ -921,10 +877,10 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
             for (int q = 0; q < 4; ++q) {
                 bf16x4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oacc[t][db][q * 4 + e] * inv);
+                for (int e = 0; e < 4; ++e) v[e] = (__bf16)(oacc[db][q * 4 + e] * inv);
                 *reinterpret_cast<bf16x4*>(op + (db * 32 + q * 8 + hh * 4) * 2) = v;
             }
-        if (p.lse && hh == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (m_run[t] * p.scale_log2 + log2f(l)) * 0.69314718055994530942f;
+        if (p.lse && hh == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (m_run * p.scale_log2 + log2f(l)) * 0.69314718055994530942f;
     }
     if (g.parts > 1) arrive<D, WAVES>(p, g, rs, sh);
     __syncthreads();
@@ -1259,21 +1215,20 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     p.cells = static_cast<unsigned long long*>(workspace);
     p.tag = (g_paged_tag.fetch_add(1, std::memory_order_relaxed) + 1) << kPgTagShift;
     const hipStream_t s = (hipStream_t)stream;
-    const dim3 block(kPgThreads);
     if (d.dtype == LOTTS_F32) {
         const dim3 grid((unsigned)((long long)d.T * d.Hq));
         // A row's keys are a chain of loads: few rows take 16 wavefronts each, so that the chain is short; many fill the chip with 4.  (80 rows of up to
-        // 700 keys 11.6 -> 8.0 us)
+        // 700 keys: 11.7 us a call with 4, 7.4 with 16.)
         if ((long long)d.T * d.Hq <= 2 * kNumCU) {
             if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 16>), grid, dim3(16 * kWave), s, p);
             else LOTTS_LAUNCH((paged_f32_kernel<128, 16>), grid, dim3(16 * kWave), s, p);
         } else {
-            if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 4>), grid, block, s, p);
-            else LOTTS_LAUNCH((paged_f32_kernel<128, 4>), grid, block, s, p);
+            if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 4>), grid, dim3(4 * kWave), s, p);
+            else LOTTS_LAUNCH((paged_f32_kernel<128, 4>), grid, dim3(4 * kWave), s, p);
         }
         return check_launch();
     }
-    const dim3 grid((unsigned)pl.workers);
+    const dim3 grid((unsigned)pl.workers), block(paged_waves<false>() * kWave);
     if (pl.wide) {
         if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, true>), grid, dim3(paged_waves<true>() * kWave), s, p);
         else LOTTS_LAUNCH((paged_attn_kernel<128, 1, true>), grid, dim3(paged_waves<true>() * kWave), s, p);

@@ -180,3 +180,47 @@ def test_replays(lotts):
         eager = torch.zeros_like(out)
         lotts.verify_attention_paged(first.Q, first.K, first.V, first.table, first.kv_len, first.q_start, out=eager, max_new=32, workspace=ws)
         assert torch.equal(eager, out)
+
+
+def test_streams_with_workspaces_of_their_own(lotts):
+    """Calls that overlap in time, one a stream, and then all of them on one stream with one workspace: the same bits."""
+    cases = [Cache(new, length, 16, 2, 128, 16, seed=i) for i, (new, length) in enumerate([((3, 1), (900, 4000)), ((300, 2), (700, 2500)), ((9, 9, 9), (100, 3000, 50))])]
+    streams = [torch.cuda.Stream() for _ in cases]
+    one = [lotts.verify_attention_paged(c.Q, c.K, c.V, c.table, c.kv_len, c.q_start, max_new=max(c.new), return_lse=True) for c in cases]
+    torch.cuda.synchronize()
+    outs = [torch.zeros_like(c.Q) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, st, o in zip(cases, streams, outs):
+            lotts.verify_attention_paged(c.Q, c.K, c.V, c.table, c.kv_len, c.q_start, max_new=max(c.new), out=o, stream=st)
+    torch.cuda.synchronize()
+    for c, (a, lse), b in zip(cases, one, outs):
+        assert torch.equal(a, b)
+        check(c, a, lse)
+
+
+def test_a_workspace_that_an_unfinished_call_left(lotts):
+    """Cells with an old tag and a count, anything in the partials: as good as zeros."""
+    c = Cache([4, 300], [3000, 1500], 16, 2, 128, 16, seed=1)
+    clean = attend(lotts, c, max_new=300)
+    ws = torch.randint(0, 2 ** 31, (64 << 20,), dtype=torch.int32, device=DEV)
+    ws[:2048] = torch.tensor([(1 << 16) + 3, 0], dtype=torch.int32, device=DEV).repeat(1024)   # 64-bit cells: tag 1, three arrivals
+    dirty = attend(lotts, c, max_new=300, workspace=ws.view(torch.uint8))
+    for a, b in zip(clean, dirty):
+        assert torch.equal(a, b)
+
+
+def test_max_new_is_a_bound_alone(lotts):
+    """Known or not, the same attention; where the most new tokens are few the lighter kernel runs, whose pieces differ."""
+    c = Cache([1, 4, 0, 2], [500, 90, 70, 1300], 8, 2, 64, 32, seed=6)
+    for most in (None, 4, 5, 7):
+        check(c, *attend(lotts, c, max_new=most))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [(1, 4), (20, 2), (300, 1)], ids=str)
+def test_a_scale_that_leaves_nothing_of_the_scores(lotts, new, dtype):
+    """Scales whose reciprocal is beyond fp32 are scales: every key weighs the same."""
+    c = Cache(new, [n + 700 for n in new], 8, 2, 128, 16, dtype, seed=8)
+    for scale in (1e-38, 2e-39):
+        check(c, *attend(lotts, c, scale=scale, max_new=max(new)), scale=scale)
