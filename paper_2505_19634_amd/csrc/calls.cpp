@@ -384,7 +384,7 @@ struct Tokens {
 };
 Tokens tokens_of(const at::Tensor& t, int64_t B, bool uniform) {
     if (t.dim() == 4 && uniform) {
-        if (t.size(0) != B || (B > 1 && t.size(1) > 0 && t.stride(0) != t.size(1) * t.stride(1))) throw Error{PyExc_ValueError, "[B][n][H][D]: the tokens must lie evenly apart"};
+        if (t.size(0) != B || (B > 1 && t.size(1) > 1 && t.stride(0) != t.size(1) * t.stride(1))) throw Error{PyExc_ValueError, "[B][n][H][D]: the tokens must lie evenly apart"};
         rows_apart(t);
         return {B * t.size(1), t.size(2), t.size(3), t.size(1) > 1 ? t.stride(1) : t.stride(0), t.stride(2)};
     }
