@@ -314,3 +314,39 @@ def test_a_generation(lotts, captured):
             assert table.max().item() < counts[1].item()
     lotts.kv_pages_free(table, refs, kv_len, page, keep=torch.zeros(B, dtype=torch.int32, device=DEV))
     assert not refs.any() and not kv_len.any() and (table == -1).all()
+
+
+def test_an_acceptance_rolls_the_lengths_back(lotts):
+    """A step as a serving loop makes it: pages for the drafts, the acceptance takes the rejected ones off kv_len, their pages are given back."""
+    B, k, V, page = 5, 3, 97, 16
+    s = State(B, 9, 60, page, 11, longest=100)
+    s.reserve(lotts, [k + 1] * B)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    zt = torch.randn(B, k + 1, V, generator=g, device=DEV)
+    zd = zt[:, :k] + torch.randn(B, k, V, generator=g, device=DEV)
+    draft = torch.randint(0, V, (B, k), generator=g, device=DEV, dtype=torch.int32)
+    n, _ = lotts.spec_accept_logits(zt, zd, draft, torch.rand(B, k + 1, generator=g, device=DEV), priv_len=s.g_len)
+    s.kv_len = [L - k + a for L, a in zip(s.kv_len, n.tolist())]
+    lotts.kv_pages_free(s.g_table, s.g_refs, s.g_len, page)
+    P.free(s.table, s.refs, s.kv_len, page)
+    s.same()
+    s.reserve(lotts, [k + 1] * B)
+
+
+def test_on_another_stream(lotts):
+    """The whole chain on a stream of its own, behind work that the current stream has nothing to do with."""
+    stream = torch.cuda.Stream()
+    s = State(4, 9, 80, 16, 12, longest=100)
+    parent = [1, 1, 0, 3]
+    stream.wait_stream(torch.cuda.current_stream())
+    lotts.kv_pages_fork(s.g_table, s.g_refs, s.g_len, gpu(parent), stream=stream)
+    torch.cuda.synchronize()   # (the argument's tensor was made on the current stream)
+    new = gpu([5, 0, 20, 1])
+    torch.cuda.synchronize()
+    copies, missing = lotts.kv_pages_reserve(s.g_table, s.g_refs, s.g_len, new, 16, stream=stream)
+    stream.synchronize()
+    P.fork(s.table, s.refs, s.kv_len, parent)
+    want, lacking = P.reserve(s.table, s.refs, s.kv_len, [5, 0, 20, 1], 16)
+    s.same()
+    assert copies.tolist() == want and missing.tolist() == [lacking]
