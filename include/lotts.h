@@ -336,7 +336,7 @@ size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc *desc);
  * chunk is exactly 0; in bf16 an infinity or NaN among the chunk's own V rows reaches the rows in front of it all the same.)
  * bf16 inputs are multiplied on the matrix cores with fp32 accumulation; fp32 inputs are computed in fp32 throughout.
  * Every call with the same data gives the same bits.  In bf16 the lengths of all branches of a call decide where a branch's keys are cut: other
- * lengths beside it may change its last bits.  Scores are taken to be below 2^29 in magnitude once scaled.
+ * lengths beside it may change its last bits.
  */
 int verify_attention_paged(const lotts_paged_desc *desc, const void *Q, const void *Kpages, const void *Vpages, const int32_t *page_table,
                            const int32_t *kv_len, const int32_t *q_start, void *O, float *lse, void *workspace, size_t workspace_bytes,
@@ -410,7 +410,7 @@ int kv_pages_compact(int32_t B, int32_t columns, int32_t pages, int32_t *page_ta
  * kv_pages_copy -- copies whole pages, in every plane (a layer's K or V) of a pool: page pairs[j][1] gets what page pairs[j][0] holds,
  * j = 0 .. n - 1, or min(n, count[0]) - 1 if count (device) is not NULL.  Pairs with a number outside [0, pages) are skipped.  No page is
  * written to that another pair of the call reads or writes.
- *   pool: planes * pages pages of page_bytes bytes (plane_stride, page_stride in BYTES); all multiples of 16, 16-byte aligned
+ *   pool: planes * pages pages of page_bytes bytes (plane_stride, page_stride in BYTES); all multiples of 16, 16-byte aligned; n * planes <= 2^36
  *   pairs [n][2] int32 (device)
  */
 int kv_pages_copy(void *pool, int32_t planes, int32_t pages, int64_t plane_stride, int64_t page_stride, int64_t page_bytes, const int32_t *pairs,

@@ -537,6 +537,7 @@ extern "C" int kv_pages_copy(void* pool, int32_t planes, int32_t pages, int64_t 
     if (planes < 1 || pages < 1 || pages > kMaxPages || n < 1 || page_bytes < 16 || page_bytes % 16 != 0 || page_bytes > (1LL << 40) ||
         page_stride < page_bytes || page_stride % 16 != 0 || plane_stride < 0 || plane_stride % 16 != 0)
         return LOTTS_ERR_SHAPE;
+    if ((long long)n * planes > (1LL << 36)) return LOTTS_ERR_SHAPE;  // pieces in 64 bits
     if (!pool || !pairs) return LOTTS_ERR_NULL;
     if (((uintptr_t)pool & 15) != 0) return LOTTS_ERR_SHAPE;
     CopyParams p;

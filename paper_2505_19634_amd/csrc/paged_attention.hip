@@ -184,7 +184,7 @@ __device__ __forceinline__ void store_out(const PagedParams& p, const Segment& g
     v[2] = (__bf16)(o.z * inv);
     v[3] = (__bf16)(o.w * inv);
     *reinterpret_cast<bf16x4*>((unsigned char*)p.O + (long long)(g.first + i) * p.o_t + h * p.o_h + c4 * 8) = v;
-    if (p.lse && c4 == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (M + log2f(l)) * 0.69314718055994530942f;
+    if (p.lse && c4 == 0) p.lse[(long long)(g.first + i) * p.Hq + h] = (M * p.scale_log2 + log2f(l)) * 0.69314718055994530942f;
 }
 
 // Merges partials [from, from + count) of the segment's item -- every STEP-th of them -- in their order: into the output, or in place of the first.
@@ -213,12 +213,12 @@ __device__ __forceinline__ void merge_parts(const PagedParams& p, const Segment&
             float Mn = M;
 #pragma unroll
             for (int j = 0; j < CH; ++j) Mn = fmaxf(Mn, ml[j].x);
-            const float Mu = Mn == -INFINITY ? 0.f : Mn, a = __builtin_amdgcn_exp2f(M - Mu);
+            const float Mu = Mn == -INFINITY ? 0.f : Mn, a = __builtin_amdgcn_exp2f((M - Mu) * p.scale_log2);
             l *= a;
             o.x *= a; o.y *= a; o.z *= a; o.w *= a;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const float w = __builtin_amdgcn_exp2f(ml[j].x - Mu);
+                const float w = __builtin_amdgcn_exp2f((ml[j].x - Mu) * p.scale_log2);
                 l += ml[j].y * w;
                 o.x += v[j].x * w; o.y += v[j].y * w; o.z += v[j].z * w; o.w += v[j].w * w;
             }
@@ -300,8 +300,8 @@ __device__ __forceinline__ float max_halves(float v) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// One row tile's step: scores of 32 keys, mask, running maximum (of the products as they are; the scale comes with the exponential) and
-// sum; the weights come back in the order in which the product with V takes them.  Register i of a lane is key (i / 4) * 8 + hh * 4 + i % 4 of
+// One row tile's step: scores of 32 keys, mask, running maximum (of the products as they are; differences from it are scaled, so that the largest
+// weight is 1 whatever the scale) and sum; the weights come back in the order in which the product with V takes them.  Register i of a lane is key (i / 4) * 8 + hh * 4 + i % 4 of
 // the tile, for row `lane % 32`; vis: keys in front of it are seen; have: bit g: 16 keys from 16 g on lie in a page.
 template <int DB>
 __device__ __forceinline__ void softmax_step(f32x16& s, f32x16 (&o)[DB], float& m, float& l, bf16x8 (&pf)[2], float scale, int vis, int have, bool masked) {
@@ -312,12 +312,12 @@ __device__ __forceinline__ void softmax_step(f32x16& s, f32x16 (&o)[DB], float& 
     float mx = m;
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    const float m_new = max_halves(mx), m_use = m_new == -INFINITY ? 0.f : m_new * scale;
-    const float alpha = __builtin_amdgcn_exp2f(m * scale - m_use);
+    const float m_new = max_halves(mx), base = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f((m - base) * scale);
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m_use));
+        const float w = __builtin_amdgcn_exp2f((s[i] - base) * scale);
         sum += w;
         pf[i >> 3][i & 7] = (__bf16)w;  // the second product takes bf16 on both sides: a half step, 2^-8 of each weight; the sum keeps fp32
     }
@@ -352,6 +352,10 @@ __device__ __forceinline__ unsigned lds_address(const void* at) {
 }
 
 constexpr int kStages = 4;     // tiles in LDS: one whose V is read, one whose K is read, two on their way
+// A wide item's weights are exp2(score * scale - maximum * scale), the latter rounded: it is kept up to 2^26, where that is a factor of 4 at most that all
+// weights of a row share.  Rows whose scores the scale takes further get a smaller scale: scores that differ by some 2^-20 of the
+// largest are 2^6 apart all the same, and the largest has all the weight.  (A difference first and then the product costs 7 % of a chunk's time.)
+constexpr float kMaxScaled = 67108864.f;
 constexpr float kRescale = 8.f;  // a running maximum may be behind the true one by a factor of 2^8 before the state is rescaled
 
 // Pieces of a tile at an address in LDS, K rows and V rows ROW bytes apart.  (What differs between the pieces of a lane lies in bits of the address that
@@ -507,7 +511,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
         if (t > 0) __syncthreads();  // the row tile before has been read
         const float l = l_run[t] + shfl_xor_f(l_run[t], 32);
         if (hh == 0) {
-            sh_m[wave][ln] = m_run[t] * p.scale_log2;
+            sh_m[wave][ln] = m_run[t];
             sh_l[wave][ln] = l;
         }
 #pragma unroll
@@ -528,7 +532,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int v = 0; v < WAVES; ++v) {
-                const float f = __builtin_amdgcn_exp2f(sh_m[v][rt] - Mu);
+                const float f = __builtin_amdgcn_exp2f((sh_m[v][rt] - Mu) * p.scale_log2);
                 const float4 ov = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds + v * SLAB) + rt * X::OSTRIDE + c4 * 4);
                 sum += sh_l[v][rt] * f;
                 o.x += ov.x * f; o.y += ov.y * f; o.z += ov.z * f; o.w += ov.w * f;
@@ -583,7 +587,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     constexpr int PAIRS = 8;                    // pairs of weights: the first half goes into the first half of the products with V
     constexpr int SPAN = QS + X::DB - (D == 64 ? 3 : 2);  // slots over which they begin: done two slots before their product
     constexpr int LOOK = QS + 2, LOOKS = VS - 3;  // slots that look at the next scores: two products behind the last one that makes them, up to the last but one
-    float negm = 0.f, mx = -INFINITY, l2 = 0.f;  // l2: the sums of every second weight
+    float row_scale = p.scale_log2, negm = 0.f, mx = -INFINITY, l2 = 0.f;  // l2: the sums of every second weight
     f32x16 sa, sb;  // scores as products leave them, in turns: of the keys that are weighed, of the next ones
     bf16x8 pf[2];
     const float scale = p.scale_log2, rescale = fminf(kRescale / scale, 3.0e38f);  // (finite however small the scale: the first maximum always counts)
@@ -592,7 +596,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     // (Every result is pinned where it is computed: the compiler would move it down to its use, behind the mask's branch.)
     auto scale_pair = [&](f32x16& c, int q) {
         const int x = q * 2;
-        float u = __builtin_fmaf(c[x], scale, negm), v = __builtin_fmaf(c[x + 1], scale, negm);
+        float u = __builtin_fmaf(c[x], row_scale, negm), v = __builtin_fmaf(c[x + 1], row_scale, negm);
         asm volatile("" : "+v"(u), "+v"(v));
         c[x] = u;
         c[x + 1] = v;
@@ -651,10 +655,12 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     auto settle = [&] {  // o and l follow where the maximum has risen much
         if (__builtin_amdgcn_ballot_w64(rise) != 0) {
             mfma_done();
-            const float m_new = rise ? mx : m, base = m_new == -INFINITY ? 0.f : m_new;
+            const float m_new = rise ? mx : m;
+            const float base = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = __builtin_amdgcn_exp2f((m - base) * scale);
             m = m_new;
-            negm = -base * scale;
+            row_scale = fabsf(base) * scale > kMaxScaled ? kMaxScaled / fabsf(base) : scale;
+            negm = -base * row_scale;
             l *= alpha;
             l2 *= alpha;
 #pragma unroll
@@ -866,7 +872,7 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 part_store4(rs, p.off_o + (at * D + db * 32 + q * 8 + hh * 4) * 4u, make_float4(oacc[db][q * 4], oacc[db][q * 4 + 1], oacc[db][q * 4 + 2], oacc[db][q * 4 + 3]));
-        if (hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run * p.scale_log2, l));
+        if (hh == 0) part_store2(rs, p.off_ml + at * 8u, make_float2(m_run, l));
     } else if (r < g.nrows) {
         const int i = quot(g.row0 + r, p.d_g), h = g.kvh * p.G + g.row0 + r - i * p.G;
         const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing is 0
@@ -1208,7 +1214,7 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     p.B = d.B; p.T = d.T; p.R = d.T / d.B; p.Hq = d.Hq; p.Hkv = d.Hkv; p.G = d.Hq / d.Hkv;
     p.pages = d.pages; p.columns = d.columns; p.shift = shift;
     const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.D);
-    p.scale_log2 = (float)(scale * 1.4426950408889634074);
+    p.scale_log2 = (float)std::min(scale * 1.4426950408889634074, 3.4e38);
     p.d_g = fast_div(p.G);
     p.items = pl.items; p.workers = pl.workers; p.part_rows = pl.part_rows;
     p.ws = workspace; p.ws_bytes = (unsigned)pl.bytes; p.off_ml = (unsigned)pl.off_ml; p.off_o = (unsigned)pl.off_o;

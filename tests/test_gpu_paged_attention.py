@@ -224,3 +224,28 @@ def test_a_scale_that_leaves_nothing_of_the_scores(lotts, new, dtype):
     c = Cache(new, [n + 700 for n in new], 8, 2, 128, 16, dtype, seed=8)
     for scale in (1e-38, 2e-39):
         check(c, *attend(lotts, c, scale=scale, max_new=max(new)), scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [(1, 4), (20, 2), (300, 1)], ids=str)
+def test_a_scale_that_leaves_one_key(lotts, new, dtype):
+    """The larger the scale, the more the largest score's key has of the weight; from some point on it has all.  Scores are whole numbers, summed without
+    rounding and all different along a row, so that the key is known and its value comes out as it is."""
+    c = Cache(new, [n + 700 for n in new], 8, 2, 128, 16, dtype, seed=9)
+    c.Q.zero_()
+    c.Q[..., :2] = 1.0
+    where = torch.arange(c.K.shape[0] * 16, device=DEV).reshape(c.K.shape[0], 16)
+    K = torch.zeros_like(c.K)
+    K[..., 0] = ((where * 37 % 4096) // 64 * 64).to(c.K.dtype)[:, None]   # multiples of 64 below 4096 and what is left: a bf16 each
+    K[..., 1] = (where * 37 % 4096 % 64).to(c.K.dtype)[:, None]
+    score = (where * 37 % 4096).tolist()
+    table, length, V = c.table.tolist(), c.kv_len.tolist(), c.V.cpu()
+    for scale in (1e3, 1e9, 1e30, 3e34):
+        out = lotts.verify_attention_paged(c.Q, K, c.V, c.table, c.kv_len, c.q_start, scale=scale, max_new=max(new)).cpu()
+        t = 0
+        for b, n in enumerate(new):
+            for i in range(n):
+                best = max(range(length[b] - n + i + 1), key=lambda k: score[table[b][k // 16]][k % 16])
+                want = V[table[b][best // 16], :, best % 16].repeat_interleave(4, dim=0)
+                assert torch.equal(out[t], want), (scale, b, i)
+                t += 1
