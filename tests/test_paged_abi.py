@@ -102,6 +102,7 @@ def test_upkeep_is_refused(lib):
     assert co(pool=None) == -1 and co(pr=None) == -1
     for bad in (dict(pl=0), dict(p=0), dict(n=0), dict(gb=0), dict(gb=24), dict(gs=8), dict(gs=(1 << 16) + 8), dict(ps=-16), dict(ps=8), dict(pool=ctypes.c_void_p(4104))):
         assert co(**bad) == -2, bad
+    assert co(n=2 ** 31 - 1, pl=33) == -2   # more pieces than 64 bits might count
 
 
 def test_binding_refuses_cpu_tensors(lib):
