@@ -310,9 +310,18 @@ __global__ __launch_bounds__(256) void kv_pages_fork_kernel(const UpkeepParams p
     const int c0 = blockIdx.x * p.cols, tid = threadIdx.x;
     const bool lengths = c0 >= p.columns;  // the last workgroup's part
     const int n = lengths ? p.B : p.B << p.log_cols;
-    for (int e = tid; e < n; e += 256) {
-        const int b = e >> p.log_cols, c = c0 + (e & (p.cols - 1));
-        old[e] = lengths ? p.kv_len[e] : c < p.columns ? p.table[b * p.table_stride + c] : -1;
+    constexpr int AT = 4;  // entries that a thread has in flight
+    for (int e0 = tid; e0 < n; e0 += AT * 256) {
+        int v[AT];
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {
+            const int e = e0 + j * 256, b = e >> p.log_cols, c = c0 + (e & (p.cols - 1));
+            v[j] = -1;
+            if (e < n) v[j] = lengths ? p.kv_len[e] : c < p.columns ? p.table[b * p.table_stride + c] : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < AT; ++j)
+            if (e0 + j * 256 < n) old[e0 + j * 256] = v[j];
     }
     for (int b = tid; b < p.B; b += 256) {
         const int from = p.arg[b];
@@ -328,7 +337,7 @@ __global__ __launch_bounds__(256) void kv_pages_fork_kernel(const UpkeepParams p
     for (int b = tid; b < p.B; b += 256)
         if (parent[b] >= 0 && parent[b] != b) atomicAdd(children + parent[b], 1);
     __syncthreads();
-    // A page gains its row's children, all at once (48 branches of one parent, one reference each: 8.4 us, at once 7.1), and loses a reference for
+    // A page gains its row's children, all at once (not one by one, so that 48 branches of one parent do not queue 48 times), and loses a reference for
     // every row that is replaced; where a row is replaced by the same page, the two meet.
     for (int e = tid; e < n; e += 256) {
         const int b = e >> p.log_cols, ci = e & (p.cols - 1), from = parent[b], was = old[e];
@@ -349,12 +358,12 @@ __global__ __launch_bounds__(kUpkeepThreads) void kv_pages_compact_kernel(const 
     int r0[kWalk];
     load_chunk(p.refs, p.pages, 0, r0);
     const int live = walk(p.refs, p.pages, p.pages + 1, counts, r0, [](int, int r) { return r > 0; }, [](int, int, bool) {});
-    load_chunk(p.refs, live, 0, r0);
+    if (p.pages > kChunk) load_chunk(p.refs, p.pages, 0, r0);  // (a pool of one chunk is in registers still)
     const int moves = walk(p.refs, live, live + 1, counts, r0, [](int, int r) { return r <= 0; },
                            [&](int i, int before, bool is) {
                                if (is) p.out[2 * before + 1] = i;
                            });
-    load_chunk(p.refs, p.pages, 0, r0);
+    if (p.pages > kChunk) load_chunk(p.refs, p.pages, 0, r0);
     walk(p.refs, p.pages, moves, counts, r0, [&](int i, int r) { return i >= live && r > 0; },
          [&](int i, int before, bool is) {
              if (is) p.out[2 * before] = i;
@@ -507,6 +516,7 @@ extern "C" int kv_pages_fork(int32_t B, int32_t columns, int32_t pages, int32_t*
     if (!kv_len || !parent) return LOTTS_ERR_NULL;
     p.kv_len = kv_len; p.arg = parent;
     p.log_cols = 6;
+    while (B << p.log_cols > 4 * 256 && p.log_cols > 2) --p.log_cols;  // one trip to memory, if that leaves 16 bytes of a row
     while (B << p.log_cols > kForkEntries) --p.log_cols;
     p.cols = 1 << p.log_cols;
     LOTTS_LAUNCH(kv_pages_fork_kernel, dim3((unsigned)((columns + (long long)p.cols - 1) / p.cols + 1)), dim3(256), (hipStream_t)stream, p);
