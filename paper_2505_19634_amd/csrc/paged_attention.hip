@@ -34,8 +34,12 @@ constexpr int kWideRows = 256;       // rows of a wide item
 constexpr int kNarrowCost = 2, kStartCost = 6;
 constexpr int wide_cost(int D) { return D == 64 ? 9 : 7; }
 constexpr int kMaxWideCost = 9;
-constexpr int kMinPiece = 32;        // places of a worker below which there are no more workers than items
+// Places of a worker below which there are no more workers than items, and for narrow items that take more than this on average: 4 tiles, one for each
+// wavefront.  (With 32 for both: 16 branches of 512 tokens 22.6 us against 13.2, 64 of 700 22.6 against 16.0, one of 2000 17.4 against 10.6; 2 tiles are
+// no faster; with 8 for both one branch of 300 tokens 9.2 against 8.3.)  A cut of a wide item moves 256 rows.
+constexpr int kMinPiece = 32, kMinNarrowPiece = 8;
 constexpr int kApartPlaces = 280;    // places of a worker below which items are cut one by one
+constexpr int kMaxWorkers = 2 * kNumCU;  // (paged_plan has when there are so many)
 constexpr int kMergeGroup = 8;       // partials that are merged at a time
 
 struct PagedParams {
@@ -896,10 +900,10 @@ template <bool WIDE>
 __host__ __device__ constexpr int paged_waves() {
     return WIDE ? 8 : 4;
 }
-template <int D, int NARROW_TILES, bool WIDE>
-__global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel(const PagedParams p) {
+template <int D, int NARROW_TILES, bool WIDE, bool TWO>
+__global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
     constexpr int WAVES = paged_waves<WIDE>();
-    constexpr int STAGES = WIDE ? 1 : 2, NARROW_LDS = WAVES * narrow_slab<D>(STAGES), WIDE_LDS = kStages * kWideTile * 2 * D * 2;
+    constexpr int STAGES = WIDE || (TWO && D == 128) ? 1 : 2, NARROW_LDS = WAVES * narrow_slab<D>(STAGES), WIDE_LDS = kStages * kWideTile * 2 * D * 2;
     __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > NARROW_LDS ? WIDE_LDS : NARROW_LDS];
     __shared__ float sh_m[WAVES][32], sh_l[WAVES][32];
     __shared__ int sh;
@@ -921,7 +925,8 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave) void paged_attn_kernel
     Pieces pieces;
     pieces.places = (double)total * p.Hkv;
     const double all = (double)number * p.Hkv;  // items
-    pieces.workers = (int)fmax(1.0, fmin(fmin((double)p.workers, pieces.places / LEAST), fmax(all, pieces.places / kMinPiece)));  // (an item's start is no reason to wait for another's)
+    const double least = !WIDE && pieces.places > kMinPiece * all ? kMinNarrowPiece : kMinPiece;
+    pieces.workers = (int)fmax(1.0, fmin(fmin((double)p.workers, pieces.places / LEAST), fmax(all, pieces.places / least)));  // (an item's start is no reason to wait for another's)
     // Short calls with wide items are cut item by item: a cut costs as much as 2 to 4 tiles (256 rows of partial outputs out and in), and a piece of the sequence
     // mostly ends one item and begins another, with a cut on either side.  Each worker gets one part of one item, of about `size` places.
     bool apart = false;
@@ -1163,7 +1168,7 @@ static std::atomic<unsigned long long> g_paged_tag{0};
 
 // Which kernel, how many workers, and where the partials lie: [arrival cells][(maximum, sum)][outputs].
 struct PagedPlan {
-    bool wide;
+    bool wide, two;
     int narrow_tiles, workers, items, part_rows;
     size_t off_ml, off_o, bytes;
 };
@@ -1172,11 +1177,15 @@ static PagedPlan paged_plan(const lotts_paged_desc& d) {
     const long long G = d.Hq / d.Hkv, rows = d.max_new * G;
     pl.wide = rows > 64;
     pl.narrow_tiles = rows > 32 ? 2 : 1;
-    pl.workers = kNumCU;
+    // Two workgroups a unit, each with one slab a wavefront at D = 128, where there are so many items that a worker has several: one's start on an item, lengths
+    // to table to keys, passes while the other works (1024 branches of 128 tokens 48.5 -> 35.1 us, 256 of 1024 51.4 -> 47, 512 of 500 55.4 ->
+    // 46).  With fewer items there would be more cuts: 16 branches x 8 heads of 4096 48.5 -> 51.2, 64 x 2 of 4096 48.5 -> 52.7.
+    pl.two = !pl.wide && pl.narrow_tiles == 1 && (long long)d.B * d.Hkv >= 2 * kNumCU;
+    pl.workers = pl.two ? 2 * kNumCU : kNumCU;
     pl.items = (int)(pl.wide ? d.T * G / kWideRows + d.B : d.B);
     pl.part_rows = (int)std::min<long long>(kWideRows, (rows + 7) / 8 * 8);
     const size_t slots = 2 * (size_t)pl.workers;
-    pl.off_ml = 4 * (size_t)pl.workers * sizeof(unsigned long long);
+    pl.off_ml = 4 * (size_t)kMaxWorkers * sizeof(unsigned long long);  // (whatever the call: the cells are nothing else, ever)
     pl.off_o = pl.off_ml + slots * pl.part_rows * 8;
     pl.bytes = pl.off_o + slots * pl.part_rows * d.D * 4;
     return pl;
@@ -1236,14 +1245,17 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     }
     const dim3 grid((unsigned)pl.workers), block(paged_waves<false>() * kWave);
     if (pl.wide) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, true>), grid, dim3(paged_waves<true>() * kWave), s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, true>), grid, dim3(paged_waves<true>() * kWave), s, p);
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
     } else if (pl.narrow_tiles == 2) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, false>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 2, false>), grid, block, s, p);
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, false, false>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 2, false, false>), grid, block, s, p);
+    } else if (pl.two) {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, false, true>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, false, true>), grid, block, s, p);
     } else {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, false>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, false>), grid, block, s, p);
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, false, false>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, false, false>), grid, block, s, p);
     }
     return check_launch();
 }

@@ -204,7 +204,7 @@ def test_a_workspace_that_an_unfinished_call_left(lotts):
     c = Cache([4, 300], [3000, 1500], 16, 2, 128, 16, seed=1)
     clean = attend(lotts, c, max_new=300)
     ws = torch.randint(0, 2 ** 31, (64 << 20,), dtype=torch.int32, device=DEV)
-    ws[:2048] = torch.tensor([(1 << 16) + 3, 0], dtype=torch.int32, device=DEV).repeat(1024)   # 64-bit cells: tag 1, three arrivals
+    ws[:4096] = torch.tensor([(1 << 16) + 3, 0], dtype=torch.int32, device=DEV).repeat(2048)   # 64-bit cells: tag 1, three arrivals
     dirty = attend(lotts, c, max_new=300, workspace=ws.view(torch.uint8))
     for a, b in zip(clean, dirty):
         assert torch.equal(a, b)
@@ -249,3 +249,29 @@ def test_a_scale_that_leaves_one_key(lotts, new, dtype):
                 want = V[table[b][best // 16], :, best % 16].repeat_interleave(4, dim=0)
                 assert torch.equal(out[t], want), (scale, b, i)
                 t += 1
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("most", [1, 5])
+def test_more_items_than_twice_the_units(lotts, D, most):
+    """More items than twice the units: two workgroups each; one branch is much longer than the others and is cut many times, some are empty."""
+    new = [(i * 7) % (most + 1) for i in range(270)]
+    length = [n + (i * 37) % 150 for i, n in enumerate(new)]
+    new[100], length[100] = most, 9000
+    c = Cache(new, length, 4, 2, D, 16, seed=D)
+    check(c, *attend(lotts, c, max_new=most))
+
+
+def test_one_workspace_for_every_kind_of_call(lotts):
+    """Calls that lay their partials out differently take turns with one buffer; all of them cut branches."""
+    many = Cache([1] * 260, [30] * 259 + [7000], 4, 2, 128, 16, seed=1)
+    cases = [(many, 1), (Cache([300, 1], [2500, 900], 8, 2, 64, 16, seed=2), 300), (Cache([4, 2], [5000, 800], 8, 2, 128, 32, seed=3), 4),
+             (Cache([12], [3000], 8, 2, 128, 16, seed=4), 12), (Cache([3, 1], [100, 60], 4, 2, 64, 16, "f32", seed=5), 3)]
+    ws = torch.zeros(80 << 20, dtype=torch.uint8, device=DEV)
+    first = [attend(lotts, c, max_new=n) for c, n in cases]
+    for a, (c, _) in zip(first, cases):
+        check(c, *a)
+    for order in (range(5), (4, 3, 2, 1, 0), (1, 0, 3, 0, 2, 0, 4, 0)):
+        for i in order:
+            again = attend(lotts, cases[i][0], max_new=cases[i][1], workspace=ws)
+            assert all(torch.equal(a, b) for a, b in zip(first[i], again)), i
