@@ -331,7 +331,8 @@ size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc *desc);
  *                 first use, then this entry point's own, shared by calls that are ordered on one stream (a captured one's replays
  *                 included: two graphs that may run at the same time have a buffer each)
  * kv_len, q_start and the table are device data and are not checked on the host: the kernels keep whatever they address inside the buffers
- * that the descriptor describes, but the rows of a branch whose data break the contract are then unspecified.
+ * that the descriptor describes.  The rows of a branch whose length is out of its range, or who has more new tokens than max_new, are then
+ * unspecified, and where q_start does not ascend within 0 .. T all rows of O are.
  * What a cache row holds behind the branch's last token does not matter, NaN included.  (A row's weight for a later token of the same
  * chunk is exactly 0; in bf16 an infinity or NaN among the chunk's own V rows reaches the rows in front of it all the same.)
  * bf16 inputs are multiplied on the matrix cores with fp32 accumulation; fp32 inputs are computed in fp32 throughout.

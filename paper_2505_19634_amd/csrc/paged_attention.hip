@@ -68,7 +68,7 @@ struct PagedParams {
 struct Branch {
     int first, n, L;
 };
-__device__ __forceinline__ Branch branch_at(const PagedParams& p, int b) {
+__host__ __device__ __forceinline__ Branch branch_at(const PagedParams& p, int b) {
     Branch r;
     int end;
     if (p.q_start) {
@@ -81,6 +81,11 @@ __device__ __forceinline__ Branch branch_at(const PagedParams& p, int b) {
     r.n = end - r.first;
     r.L = min(max(p.kv_len[b], 0), p.columns << p.shift);
     return r;
+}
+// Keys that row t of Q sees if it is one of the branch's new tokens, never more than the branch has; -1 if it is not: where q_start does not ascend,
+// a search for the branch that t belongs to may end at one that does not hold it.
+__host__ __device__ __forceinline__ int keys_of_row(const Branch& br, int t) {
+    return t < br.first || t - br.first >= br.n ? -1 : max(0, br.L - br.n + (t - br.first) + 1);
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* base, unsigned bytes) {
@@ -1049,9 +1054,8 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
         b = t / p.R;
     }
     b = __builtin_amdgcn_readfirstlane(b);
-    const Branch br = branch_at(p, b);
-    if (t < br.first) return;
-    const int n = max(0, br.L - br.n + (t - br.first) + 1);
+    const int n = keys_of_row(branch_at(p, b), t);
+    if (n < 0) return;
     const float scale = p.scale_log2 * 0.69314718055994530942f;
     const float4 qv = *reinterpret_cast<const float4*>((const unsigned char*)p.Q + t * p.q_t + h * p.q_h + c4 * 16);
     const int32_t* row = p.table + b * p.table_stride;
