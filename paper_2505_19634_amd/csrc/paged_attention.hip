@@ -52,6 +52,7 @@ struct PagedParams {
     int items;                          // item slots of a KV head
     int workers;
     float scale_log2;                   // scale * log2(e)
+    float scale;
     FastDiv d_g;
     void* O;
     float* lse;
@@ -1029,7 +1030,8 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) v
 // ---------------------------------------------------------------------------------------------
 // fp32: fp32 arithmetic throughout, a workgroup per row of a head.  A key row is D / 4 lanes of 16 bytes; a wavefront takes every
 // WAVES-th chunk of 4 * 256 / D keys (no chunk is larger than 16 keys: it lies in one page) and keeps a running state per D / 4 lanes;
-// the states meet at the end.
+// the states meet at the end.  The maximum is that of the scores as they are and the differences from it are scaled, so that the largest weight is 1
+// whatever the scale.
 // ---------------------------------------------------------------------------------------------
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedParams p) {
@@ -1056,7 +1058,7 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
     b = __builtin_amdgcn_readfirstlane(b);
     const int n = keys_of_row(branch_at(p, b), t);
     if (n < 0) return;
-    const float scale = p.scale_log2 * 0.69314718055994530942f;
+    const float scale = p.scale;
     const float4 qv = *reinterpret_cast<const float4*>((const unsigned char*)p.Q + t * p.q_t + h * p.q_h + c4 * 16);
     const int32_t* row = p.table + b * p.table_stride;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1080,16 +1082,16 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
             s[i] = qv.x * kv[i].x + qv.y * kv[i].y + qv.z * kv[i].z + qv.w * kv[i].w;
 #pragma unroll
             for (int d = LPK / 2; d >= 1; d >>= 1) s[i] += shfl_xor_f(s[i], d);
-            s[i] = j0 + i * KPL + grp < n ? s[i] * scale : -INFINITY;
+            s[i] = j0 + i * KPL + grp < n ? s[i] : -INFINITY;
             mx = fmaxf(mx, s[i]);
         }
         const float mu = mx == -INFINITY ? 0.f : mx;
-        const float alpha = expf(m - mu);
+        const float alpha = expf((m - mu) * scale);
         l *= alpha;
         acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
 #pragma unroll
         for (int i = 0; i < NJ; ++i) {
-            const float pv = expf(s[i] - mu);
+            const float pv = expf((s[i] - mu) * scale);
             if (j0 + i * KPL + grp >= n) vv[i] = make_float4(0.f, 0.f, 0.f, 0.f);  // an infinity counts once
             l += pv;
             acc.x += pv * vv[i].x; acc.y += pv * vv[i].y; acc.z += pv * vv[i].z; acc.w += pv * vv[i].w;
@@ -1101,7 +1103,7 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
         const float mo = shfl_xor_f(m, d), lo = shfl_xor_f(l, d);
         const float4 ao = make_float4(shfl_xor_f(acc.x, d), shfl_xor_f(acc.y, d), shfl_xor_f(acc.z, d), shfl_xor_f(acc.w, d));
         const float M = fmaxf(m, mo);
-        const float wa = m == -INFINITY ? 0.f : expf(m - M), wb = mo == -INFINITY ? 0.f : expf(mo - M);
+        const float wa = m == -INFINITY ? 0.f : expf((m - M) * scale), wb = mo == -INFINITY ? 0.f : expf((mo - M) * scale);
         l = l * wa + lo * wb;
         acc.x = acc.x * wa + ao.x * wb; acc.y = acc.y * wa + ao.y * wb; acc.z = acc.z * wa + ao.z * wb; acc.w = acc.w * wa + ao.w * wb;
         m = M;
@@ -1119,12 +1121,12 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
         float lsum = 0.f, o = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float wgt = (sh_ml[w][0] == -INFINITY) ? 0.f : expf(sh_ml[w][0] - M);
+            const float wgt = (sh_ml[w][0] == -INFINITY) ? 0.f : expf((sh_ml[w][0] - M) * scale);
             lsum += sh_ml[w][1] * wgt;
             o += sh_acc[w][tid] * wgt;
         }
         reinterpret_cast<float*>((unsigned char*)p.O + t * p.o_t + h * p.o_h)[tid] = lsum == 0.f ? 0.f : o / lsum;
-        if (p.lse && tid == 0) p.lse[(long long)t * p.Hq + h] = M + logf(lsum);
+        if (p.lse && tid == 0) p.lse[(long long)t * p.Hq + h] = M * scale + logf(lsum);
     }
 }
 
@@ -1227,6 +1229,7 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     p.B = d.B; p.T = d.T; p.R = d.T / d.B; p.Hq = d.Hq; p.Hkv = d.Hkv; p.G = d.Hq / d.Hkv;
     p.pages = d.pages; p.columns = d.columns; p.shift = shift;
     const double scale = d.scale > 0.0f ? (double)d.scale : 1.0 / sqrt((double)d.D);
+    p.scale = (float)scale;
     p.scale_log2 = (float)std::min(scale * 1.4426950408889634074, 3.4e38);
     p.d_g = fast_div(p.G);
     p.items = pl.items; p.workers = pl.workers; p.part_rows = pl.part_rows;
