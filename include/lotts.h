@@ -307,7 +307,8 @@ typedef struct {
     int64_t o_stride_t, o_stride_h;                           /* O [T][Hq][D] */
 } lotts_paged_desc;
 
-/* Bytes of workspace verify_attention_paged needs for this geometry; 0 if the descriptor is invalid. */
+/* Bytes of workspace verify_attention_paged needs for this geometry; 0 if the descriptor is invalid.  Never less for more branches (B) or more new
+ * tokens (T, max_new) with the same heads and type: a buffer for the largest call serves the smaller ones. */
 size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc *desc);
 
 /*

@@ -1193,7 +1193,9 @@ static PagedPlan paged_plan(const lotts_paged_desc& d) {
     const size_t slots = 2 * (size_t)pl.workers;
     pl.off_ml = 4 * (size_t)kMaxWorkers * sizeof(unsigned long long);  // (whatever the call: the cells are nothing else, ever)
     pl.off_o = pl.off_ml + slots * pl.part_rows * 8;
-    pl.bytes = pl.off_o + slots * pl.part_rows * d.D * 4;
+    // A workspace for more branches and more new tokens serves fewer: twice the workers' partials of up to 32 rows are more than the partials of 33 to 56.
+    const size_t at_least = (long long)d.B * d.Hkv >= 2 * kNumCU ? 2 * (size_t)kMaxWorkers * std::min(pl.part_rows, 32) : 0;
+    pl.bytes = pl.off_ml + std::max(slots * pl.part_rows, at_least) * (8 + (size_t)d.D * 4);
     return pl;
 }
 
