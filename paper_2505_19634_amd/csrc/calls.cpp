@@ -348,6 +348,15 @@ long device_of(PyObject* o) {
     }
     return d;
 }
+int32_t page_of(PyObject* o) {
+    const long n = PyLong_AsLong(o);
+    if (n == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Error{PyExc_TypeError, "page_tokens must be a number"};
+    }
+    if (n != (int32_t)n) throw Error{PyExc_ValueError, "page_tokens must be a power of two from 16 to 1024"};
+    return (int32_t)n;
+}
 // Whole numbers: dense, at least n of them.
 int32_t* numbers(const at::Tensor& t, int64_t n, const char* what) {
     if (!is(t, at::kInt)) throw Error{PyExc_TypeError, what};
@@ -361,6 +370,7 @@ struct Table {
 Table table_of(const at::Tensor& t) {
     if (t.scalar_type() != at::kInt) throw Error{PyExc_TypeError, "page_table must be int32"};
     if (t.dim() != 2 || t.stride(1) != 1 || (t.size(0) > 1 && t.stride(0) < t.size(1))) throw Error{PyExc_ValueError, "page_table must be [B][columns] with rows apart"};
+    if (t.size(0) > 0x7fffffff || t.size(1) > 0x7fffffff) throw Error{PyExc_ValueError, "page_table is too large"};
     return {static_cast<int32_t*>(t.data_ptr()), (int32_t)t.size(0), (int32_t)t.size(1), t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), t.size(1))};
 }
 int32_t paged_dtype(const at::Tensor& t) {
@@ -418,6 +428,7 @@ PyObject* call_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
             PyErr_Clear();
             throw Error{PyExc_TypeError, "max_new and scale must be numbers"};
         }
+        if (scale != 0.0 && (float)scale == 0.0f) throw Error{PyExc_ValueError, "the scale is nothing in float32"};  // (where 0 selects 1 / sqrt(D))
         if (most < 0 || most > 0x7fffffff) most = 0;
         if (uniform && most * tab.B != q.T) throw Error{PyExc_ValueError, "without q_start every branch has T / B new tokens"};
         float* lse = nullptr;
@@ -491,7 +502,7 @@ PyObject* call_reserve(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         const Upkeep u = upkeep_of(on, a[0], a[1]);
         int32_t* len = numbers(on(a[2], "kv_len must be a tensor"), u.tab.B, "kv_len must be contiguous int32 [B]");
         const int32_t* more = numbers(on(a[3], "new_tokens must be a tensor"), u.tab.B, "new_tokens must be contiguous int32 [B]");
-        const int32_t page = (int32_t)device_of(a[4]);
+        const int32_t page = page_of(a[4]);
         int32_t* copies = numbers(on(a[5], "copies must be a tensor"), 2 * (int64_t)u.tab.B, "copies must be contiguous int32 [B][2]");
         int32_t* missing = numbers(on(a[6], "missing must be a tensor"), 1, "missing must be contiguous int32 [1]");
         const size_t need = 4 * (size_t)u.pages;
@@ -526,7 +537,7 @@ PyObject* call_free(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         const OneDevice on{device_of(a[5])};
         const Upkeep u = upkeep_of(on, a[0], a[1]);
         int32_t* len = numbers(on(a[2], "kv_len must be a tensor"), u.tab.B, "kv_len must be contiguous int32 [B]");
-        const int32_t page = (int32_t)device_of(a[3]);
+        const int32_t page = page_of(a[3]);
         const int32_t* keep = a[4] == Py_None ? nullptr : numbers(on(a[4], "keep must be a tensor"), u.tab.B, "keep must be contiguous int32 [B]");
         void* stream = address(a[6]);
         return released([&] { return c->release(u.tab.B, u.tab.columns, u.pages, page, u.tab.entries, u.tab.stride, u.refs, len, keep, stream); });
