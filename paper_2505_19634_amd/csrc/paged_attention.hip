@@ -569,14 +569,21 @@ __device__ constexpr int wide_loads() {
 
 // The products of a wide item are written as instructions, on vector registers, so that a slot of the loop below holds what it was given.  (Left to choose, the
 // compiler put the scores into accumulation registers, Q into scratch memory and the waits for that into the loop.)  It does not know how long
-// these take: what reads a result on the vector units is kept behind two later products, or behind mfma_done().
+// these take: what reads a result on the vector units is kept behind two later products, or behind mfma_done(), which hands the result on (a wait
+// without it is no reason for the compiler to keep what reads the result behind the wait).
 __device__ __forceinline__ void mfma_first(f32x16& d, const bf16x8& a, const bf16x8& b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_onto(f32x16& d, const bf16x8& a, const bf16x8& b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
 }
-__device__ __forceinline__ void mfma_done() { asm volatile("s_nop 15\n\ts_nop 15"); }
+__device__ __forceinline__ void mfma_done(f32x16& d) { asm volatile("s_nop 15\n\ts_nop 15" : "+v"(d)); }
+template <int N>
+__device__ __forceinline__ void mfma_done(f32x16 (&d)[N]) {
+    static_assert(N == 2 || N == 4, "blocks of the head dimension");
+    if constexpr (N == 2) asm volatile("s_nop 15\n\ts_nop 15" : "+v"(d[0]), "+v"(d[1]));
+    else asm volatile("s_nop 15\n\ts_nop 15" : "+v"(d[0]), "+v"(d[1]), "+v"(d[2]), "+v"(d[3]));
+}
 
 // The loop over a wide item's tiles for a wavefront with a row tile.  arrive(): the next tile is in LDS for everybody; request(j, v, i): load i of the
 // wavefront's part of tile j's K or V.  In a step 32 keys are weighed and multiplied with V while the next 32 are multiplied with Q and their maximum
@@ -651,7 +658,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     };
     auto mask = [&](f32x16& n, int kb, int have) {
         if ((have & 3) == 3 && kb + 32 <= first_lim) return;
-        mfma_done();
+        mfma_done(n);
         const int hh = (threadIdx.x & 32) >> 5;
         const int vis = lim - kb - hh * 4;
 #pragma unroll
@@ -664,7 +671,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
     };
     auto settle = [&] {  // o and l follow where the maximum has risen much
         if (__builtin_amdgcn_ballot_w64(rise) != 0) {
-            mfma_done();
+            mfma_done(o);
             const float m_new = rise ? mx : m;
             const float base = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = __builtin_amdgcn_exp2f((m - base) * scale);
@@ -741,7 +748,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
             const bf16x8 v = read_v(st, i);
             multiply_v(i, v);
         }
-        mfma_done();
+        mfma_done(o);
     };
     have = arrive(true);
 #pragma unroll
@@ -751,7 +758,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         const bf16x8 k = read_k(st, i);
         multiply_k(sa, i, k);
     }
-    mfma_done();
+    mfma_done(sa);
     mask(sa, lo * kWideTile, have);
 #pragma unroll
     for (int r = 0; r < PAIRS; ++r) look(sa, r);
