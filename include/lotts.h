@@ -334,8 +334,8 @@ size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc *desc);
  * kv_len, q_start and the table are device data and are not checked on the host: the kernels keep whatever they address inside the buffers
  * that the descriptor describes.  The rows of a branch whose length is out of its range, or who has more new tokens than max_new, are then
  * unspecified, and where q_start does not ascend within 0 .. T all rows of O are.
- * What a cache row holds behind the branch's last token does not matter, NaN included.  (A row's weight for a later token of the same
- * chunk is exactly 0; in bf16 an infinity or NaN among the chunk's own V rows reaches the rows in front of it all the same.)
+ * What a cache row holds behind the branch's last token does not matter, NaN included, and an infinity or NaN in V reaches the rows that see its
+ * key and no others (from a chunk's own tokens as NaN in bf16).
  * bf16 inputs are multiplied on the matrix cores with fp32 accumulation; fp32 inputs are computed in fp32 throughout.
  * Every call with the same data gives the same bits.  In bf16 the lengths of all branches of a call decide where a branch's keys are cut: other
  * lengths beside it may change its last bits.

@@ -395,10 +395,66 @@ __device__ __forceinline__ bf16x8 read_v(unsigned at, int kk, int db) {  // A op
     return f.v;
 }
 
+// Infinities and NaN in V.  A row's weight for a later token of its chunk is 0, but the product with V takes it all the same, and 0 times an infinity is
+// NaN.  So where some rows of an item do not see a key, what is not finite in the key's row of V is taken out of LDS before the products, and the rows that
+// see it get NaN in its columns afterwards.  (Looking costs the drafts of 16 branches 0.2 %, a prompt of 2039 0.8 %, one of 1500 with as many KV heads as
+// query heads 2.3 %, 31.4 us for 30.7; with NaN all over V these take 53, 58 and 85 us.  Adding the values themselves, by conditions an element, made the
+// wide kernels 10 KB larger and a prompt 2 us slower.)
+__device__ __forceinline__ unsigned not_finite(unsigned two) {  // bits 15 and 31: of a bf16 whose exponent's bits are all set
+    return ((two & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+// 16 bytes of every lane, at an address in LDS; whether anything was taken out.
+__device__ __forceinline__ bool keep_finite(unsigned at) {
+    __attribute__((address_space(3))) u32x4* piece = (__attribute__((address_space(3))) u32x4*)(uintptr_t)at;
+    u32x4 v = *piece;
+    if (__builtin_expect(__ballot((not_finite(v[0]) | not_finite(v[1]) | not_finite(v[2]) | not_finite(v[3])) != 0) == 0, 1)) return false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] &= ~((not_finite(v[i]) >> 15) * 0xffffu);
+    *piece = v;
+    return true;
+}
+// Columns of V that the lane looks after, and the first key in whose row they are not finite.
+template <int D>
+struct NotFinite {
+    static constexpr int C = D / kWave;
+    int first[C];
+    __device__ __forceinline__ NotFinite() {
+#pragma unroll
+        for (int i = 0; i < C; ++i) first[i] = 0x7fffffff;
+    }
+    __device__ __forceinline__ void look(const PagedParams& p, const int32_t* row, int kvh, int from, int to) {  // the later, the larger the keys
+#pragma unroll 4
+        for (int key = from; key < to; ++key) {
+            const int e = page_entry(p, row, key);
+            const bool there = (unsigned)e < (unsigned)p.pages;  // (in no page: that of page 0 is read for nothing)
+            const unsigned short* v = reinterpret_cast<const unsigned short*>((const unsigned char*)p.V + group_at(p, e, key, kvh)) + (threadIdx.x & (kWave - 1)) * C;
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+                if (there && (v[i] & 0x7f80) == 0x7f80) first[i] = min(first[i], key);
+        }
+    }
+    // at: D words of LDS that are the wavefront's.
+    __device__ __forceinline__ void publish(unsigned at) const {
+#pragma unroll
+        for (int i = 0; i < C; ++i) *(__attribute__((address_space(3))) int*)(uintptr_t)(at + ((threadIdx.x & (kWave - 1)) * C + i) * 4) = first[i];
+    }
+    // The outputs of the lane's row, which sees the keys in front of lim.
+    static __device__ __forceinline__ void mark(unsigned at, int lim, f32x16 (&o)[D / 32]) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const u32x4 k = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(at + (db * 32 + q * 8 + (threadIdx.x & 32) / 8) * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[db][q * 4 + i] = (int)k[i] < lim ? NAN : o[db][q * 4 + i];
+            }
+    }
+};
+
 // A narrow item's part: wavefront w takes tiles lo + w, lo + w + WAVES, ..., through STAGES slabs of its own: with two, the next tile is on its way while
 // one is worked on; with one, the other wavefronts' are.
 template <int D, int TW, int WAVES, int STAGES>
-__device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh) {
+__device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh_bad, int (*sh_first)[D], int* sh) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kNarrowTile * ROW, SLAB = narrow_slab<D>(STAGES), LOADS = 4 * X::NLD;  // of a tile
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
@@ -460,6 +516,8 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
         for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
     }
     const bool two = TW > 1 && g.nrows > 32;
+    bool taken_out = false;
+    const int unseen = g.n > 1 ? (before + 1) & -X::RPI : 0x7fffffff;  // keys that not all rows see, and those that a load brings with them
     const unsigned kat = slab + lane_of_k<D>(lane), vat = slab + HALF + lane_of_v<D>(lane);
     f32x16 oacc[TW][X::DB];
     float m_run[TW], l_run[TW];
@@ -481,6 +539,11 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        if (__builtin_expect(kb + kNarrowTile > unseen, 0)) {
+#pragma unroll 1
+            for (int key = max(kb, unseen); key < min(kb + kNarrowTile, keys); key += X::RPI)
+                taken_out |= keep_finite(slab + stage + HALF + (key - kb) * ROW + lane * 16);
         }
         const bool masked = have != 3 || kb + kNarrowTile > before + 1;
         bf16x8 kf[X::KS], pf[TW][2];
@@ -510,6 +573,16 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             have_next = fetch(it + 1);
         }
     }
+    if (__builtin_expect(taken_out, 0)) {
+        NotFinite<D> bad;
+#pragma unroll 1
+        for (int it = 0; it < n_tiles; ++it) {
+            const int kb = (g.lo + wave + it * WAVES) * kNarrowTile;
+            bad.look(p, row, g.kvh, max(kb, unseen), min(kb + kNarrowTile, keys));
+        }
+        bad.publish(lds_address(sh_first[wave]));
+    }
+    sh_bad[wave] = taken_out;
     // the wavefronts' states of a row tile meet in LDS, in their order
     const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
     constexpr int F4 = D / 4, QPT = 32 * F4 / (WAVES * kWave), RSTEP = WAVES * kWave / F4;
@@ -531,6 +604,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
                 *reinterpret_cast<float4*>(obuf + ln * X::OSTRIDE + db * 32 + q * 8 + hh * 4) =
                     make_float4(oacc[t][db][q * 4], oacc[t][db][q * 4 + 1], oacc[t][db][q * 4 + 2], oacc[t][db][q * 4 + 3]);
         __syncthreads();
+        const bool any_bad = __ballot(sh_bad[lane % WAVES] != 0) != 0;
 #pragma unroll
         for (int q = 0; q < QPT; ++q) {
             const int rt = row0 + q * RSTEP, r = t * 32 + rt;
@@ -546,6 +620,18 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
                 const float4 ov = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds + v * SLAB) + rt * X::OSTRIDE + c4 * 4);
                 sum += sh_l[v][rt] * f;
                 o.x += ov.x * f; o.y += ov.y * f; o.z += ov.z * f; o.w += ov.w * f;
+            }
+            if (__builtin_expect(any_bad, 0)) {
+                const int sees = before + quot(r, p.d_g) + 1;
+#pragma unroll 1
+                for (int v = 0; v < WAVES; ++v) {
+                    if (!sh_bad[v]) continue;
+                    const int4 k = *reinterpret_cast<const int4*>(&sh_first[v][c4 * 4]);
+                    o.x = k.x < sees ? NAN : o.x;
+                    o.y = k.y < sees ? NAN : o.y;
+                    o.z = k.z < sees ? NAN : o.z;
+                    o.w = k.w < sees ? NAN : o.w;
+                }
             }
             if (g.parts == 1) {
                 store_out(p, g, r, c4, o, M, sum);
@@ -716,9 +802,9 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         }
         if (D == 64) asm volatile("s_nop 1");  // (the first half's last weights were rounded in the slot before)
         mask(n, j * 32, have);
-        // the tile of the next step's K, so that its first pieces are read beside the products with V
-        if ((j & 1) != 0 && j + 1 < 2 * hi) have = arrive(false) << 2;
         const unsigned after = ((j + 1) >> 1) % kStages * STAGE + ((j + 1) & 1) * 32 * ROW;
+        // the tile of the next step's K, so that its first pieces are read beside the products with V
+        if ((j & 1) != 0 && j + 1 < 2 * hi) have = arrive(false, after) << 2;
 #pragma unroll
         for (int i = 0; i < VS; ++i) {
             __builtin_amdgcn_sched_barrier(0);
@@ -750,7 +836,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         }
         mfma_done(o);
     };
-    have = arrive(true);
+    have = arrive(true, st);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) request(lo + 2, 0, i);
 #pragma unroll
@@ -777,7 +863,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
 
 // The workgroup loads a tile together, 8 keys a wavefront; wavefront w takes row tile w of the item.
 template <int D, int WAVES>
-__device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, unsigned char* lds, int* sh) {
+__device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, unsigned char* lds, int* sh, int* sh_bad) {
     using X = Tile<D>;
     constexpr int KEYS = kWideTile / WAVES, LOADS = wide_loads<D>();
     static_assert(WAVES * 32 == kWideRows && KEYS * WAVES == kWideTile && KEYS <= kPgGroup && KEYS == LOADS * X::RPI, "a row tile and some keys of a tile for every wavefront");
@@ -832,6 +918,9 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         load_to_lds<false>(buffer((const unsigned char*)p.K + (long long)(at + (k_to_v & (unsigned long long)-(long long)v)), bytes), row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (first ^ spread<D>(i * X::RPI) * 16),
                     stage + v * HALF + i * 1024);
     };
+    const int unseen = (before + quot(g.row0, p.d_g) + 1) & -KEYS;  // keys that not all rows see, and those that a wavefront loads with them
+    int until_unseen = max(0, (unseen - wave * KEYS + kWideTile - 1) / kWideTile) - g.lo;  // tiles to arrive in front of the first one in which the wavefront has such keys
+    sh_bad[wave] = 0;  // (whether the wavefront has taken something out of V)
     look_ahead(g.lo);
 #pragma unroll
     for (int tile = 0; tile < 2; ++tile) {
@@ -843,7 +932,15 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     }
     // The next tile is in LDS for everybody; everybody has left the tile before the last behind, whose stage the next requests take.  Loads behind
     // the tile's that are on their way: K and V of the next one at first, then K and half of V of the next one.
-    auto arrive_tile = [&](bool first) {
+    auto arrive_tile = [&](bool first, unsigned stage_at) {
+        if (__builtin_expect(--until_unseen < 0, 0)) {
+            if (first) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS + LOADS / 2) : "memory");
+            bool taken_out = false;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) taken_out |= keep_finite(to + stage_at + HALF + i * 1024 + lane * 16);
+            if (taken_out) sh_bad[wave] = 1;
+        }
         if (first) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS + LOADS / 2) : "memory");
         const int have = have_0;
@@ -865,13 +962,13 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     if (wave * 32 < g.nrows) {
         wide_rows<D>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
     } else {  // no rows: the loads and the meetings alone, in the same order
-        arrive_tile(true);
+        arrive_tile(true, g.lo % kStages * STAGE);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) request(g.lo + 2, 0, i);
         for (int j = g.lo; j + 1 < g.hi; ++j) {
 #pragma unroll
             for (int i = 0; i < LOADS / 2; ++i) request(j + 2, 1, i);
-            arrive_tile(false);
+            arrive_tile(false, (j + 1) % kStages * STAGE);
 #pragma unroll
             for (int i = LOADS / 2; i < LOADS; ++i) request(j + 2, 1, i);
 #pragma unroll
@@ -879,6 +976,14 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // (everybody has met behind the last tile that anything was taken out of)
+    if (__builtin_expect(__ballot(sh_bad[lane & (WAVES - 1)] != 0) != 0, 0)) {
+        NotFinite<D> bad;
+        bad.look(p, row, g.kvh, max(g.lo * kWideTile, unseen), min(g.hi * kWideTile, keys));
+        __syncthreads();  // (the tiles have been read)
+        bad.publish(lds_address(lds) + wave * D * 4);
+        NotFinite<D>::mark(lds_address(lds) + wave * D * 4, lim, oacc);
+    }
     const __amdgpu_buffer_rsrc_t rs = buffer(p.ws, p.ws_bytes);
     const float l = l_run + shfl_xor_f(l_run, 32);
     const int r = wave * 32 + ln;
@@ -919,7 +1024,8 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) v
     constexpr int STAGES = WIDE || (TWO && D == 128) ? 1 : 2, NARROW_LDS = WAVES * narrow_slab<D>(STAGES), WIDE_LDS = kStages * kWideTile * 2 * D * 2;
     __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > NARROW_LDS ? WIDE_LDS : NARROW_LDS];
     __shared__ float sh_m[WAVES][32], sh_l[WAVES][32];
-    __shared__ int sh;
+    __shared__ int sh, sh_bad[WAVES];  // sh_bad: whether a wavefront has taken something out of V; sh_first: NotFinite's, of a narrow item
+    __shared__ __attribute__((aligned(16))) int sh_first[WAVES][D];
     const int lane = threadIdx.x & (kWave - 1);
     const int per_xcd = p.workers / kNumXCD;  // neighbours in the sequence share an XCD and with it a KV head's keys in its L2
     const int w = (int)(blockIdx.x % kNumXCD) * per_xcd + (int)(blockIdx.x / kNumXCD);
@@ -1026,10 +1132,10 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) v
         g.hi = __builtin_amdgcn_readfirstlane(g.hi);
         if (g.lo >= g.hi) continue;
         if constexpr (WIDE) {
-            if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
-            else wide_segment<D, WAVES>(p, g, lds, &sh);
+            if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
+            else wide_segment<D, WAVES>(p, g, lds, &sh, sh_bad);
         } else {
-            narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, &sh);
+            narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
         }
     }
 }
