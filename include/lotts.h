@@ -293,14 +293,15 @@ int skinny_gemm_append(int32_t B, int32_t k, int32_t Hkv, int32_t D, int32_t N, 
 typedef struct {
     int32_t B;            /* branches, 1 .. 4096 */
     int32_t T;            /* rows of Q and O: new tokens of all branches together, >= 1; T * Hq < 2^24 */
-    int32_t max_new;      /* no branch has more new tokens than this; 1 <= max_new <= T */
+    int32_t max_new;      /* no branch has more new tokens than this; 1 <= max_new <= T.  A close bound is worth having: the kernel and its
+                           * workspace go by it, and with max_new * Hq / Hkv > 64 they are those of long chunks */
     int32_t Hq, Hkv;      /* query / KV heads, Hq % Hkv == 0; query head h reads KV head h / (Hq / Hkv) */
     int32_t D;            /* head dimension: 64 or 128 */
     int32_t page_tokens;  /* tokens of a page: a power of two from 16 to 1024 */
     int32_t pages;        /* pages of the pool, 1 .. 2^24 */
     int32_t columns;      /* entries of a branch's row of the table; columns * page_tokens < 2^30 */
     int32_t dtype;        /* lotts_dtype of Q, K, V and O */
-    float scale;          /* softmax scale; 0 selects 1 / sqrt(D) */
+    float scale;          /* softmax scale, up to 3e38 (bf16: from 2.35e38 on as that); 0 selects 1 / sqrt(D) */
     int64_t q_stride_t, q_stride_h;                           /* Q [T][Hq][D] */
     int64_t page_stride_p, page_stride_h, page_stride_t;      /* Kpages, Vpages [pages][Hkv][page_tokens][D] */
     int64_t table_stride;                                     /* page_table [B][columns] */
@@ -374,11 +375,15 @@ size_t kv_pages_workspace_bytes(int32_t pages);
 /*
  * kv_pages_reserve -- room for new_tokens[b] (>= 0) more tokens of every branch, whose lengths grow by as many.  Every page that they will be
  * written to is the branch's alone afterwards: where the table has none, and where the page is shared, it gets a free one (the
- * free pages with the lowest numbers, in the order of branches and columns).  A shared page that holds tokens to keep has to be copied:
- * copies[b] = (from, to), at most one a branch, (-1, -1) for none; kv_pages_copy takes them as they are, before the next call that
- * changes the state.
- *   copies [B][2] int32 out;  missing [1] int32 out: 0, or nothing has been changed: > 0, so many free pages were lacking; -1, a
- *   branch's tokens would pass the table's columns
+ * free pages with the lowest numbers, in the order of branches and columns).  Where all that share a page are written to in one call, each of them gets
+ * a page and the shared one is free afterwards: it counts among those that are lacking while they are handed out.  A shared page that holds
+ * tokens to keep has to be copied: copies[b] = (from, to), at most one a branch, (-1, -1) for none; kv_pages_copy takes them as they are, before the
+ * next call that changes the state.
+ *   copies [B][2] int32 out;  missing [1] int32 out: 0, or the state has not been changed (and copies holds none): > 0, so many free pages were
+ *   lacking; -1, a branch's tokens would pass the table's columns
+ * The lengths have not grown then, so that the new tokens have no place: a kv_append_paged behind it would write them over the last tokens of
+ * their branches, in pages that others may share.  A program that enqueues both without reading `missing` in between, or captures them
+ * together, needs a pool and a table that always have room.
  */
 int kv_pages_reserve(int32_t B, int32_t columns, int32_t pages, int32_t page_tokens, int32_t *page_table, int64_t table_stride, int32_t *refs,
                      int32_t *kv_len, const int32_t *new_tokens, int32_t *copies, int32_t *missing, void *workspace, size_t workspace_bytes,
@@ -401,7 +406,8 @@ int kv_pages_free(int32_t B, int32_t columns, int32_t pages, int32_t page_tokens
 
 /*
  * kv_pages_compact -- the pages in use become pages 0 .. n - 1, n their number: those from n on, in ascending order, take the places of the
- * free ones below n, in ascending order; table and references follow.  The data move by kv_pages_copy with the same pairs.
+ * free ones below n, in ascending order; table and references follow.  The data move by kv_pages_copy with the same pairs.  (A table entry
+ * that names a page without references, which these calls never leave, becomes -1 from n on; below n it stays, and may then name another's page.)
  *   moves [max(1, pages / 2)][2] int32 out: (from, to); rows behind the last pair are left as they were
  *   counts [2] int32 out: number of pairs, n
  */

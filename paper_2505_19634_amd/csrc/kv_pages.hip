@@ -368,7 +368,7 @@ __global__ __launch_bounds__(kUpkeepThreads) void kv_pages_compact_kernel(const 
          [&](int i, int before, bool is) {
              if (is) p.out[2 * before] = i;
          });
-    for (int i = live + tid; i < p.pages; i += kUpkeepThreads) p.list[i] = -1;  // an entry that names a free page names none afterwards
+    for (int i = live + tid; i < p.pages; i += kUpkeepThreads) p.list[i] = -1;  // an entry from `live` on that names a free page names none afterwards
     __syncthreads();
     for (int j = tid; j < moves; j += kUpkeepThreads) {
         const int src = p.out[2 * j], dst = p.out[2 * j + 1];

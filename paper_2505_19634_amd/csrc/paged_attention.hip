@@ -92,7 +92,7 @@ __host__ __device__ __forceinline__ int keys_of_row(const Branch& br, int t) {
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* base, unsigned bytes) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
 }
-// Partials cross workgroups inside the launch: device scope (sc0 sc1).
+// Partials cross workgroups, and with them XCDs, inside the launch: sc0 sc1, past every cache that is not shared (system scope; device scope is sc1 alone).
 constexpr int kDevScope = 17;
 __device__ __forceinline__ void part_store4(__amdgpu_buffer_rsrc_t r, unsigned at, float4 v) {
     u32x4 u;
@@ -1047,7 +1047,11 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) v
     const double least = !WIDE && pieces.places > kMinPiece * all ? kMinNarrowPiece : kMinPiece;
     pieces.workers = (int)fmax(1.0, fmin(fmin((double)p.workers, pieces.places / LEAST), fmax(all, pieces.places / least)));  // (an item's start is no reason to wait for another's)
     // Short calls with wide items are cut item by item: a cut costs as much as 2 to 4 tiles (256 rows of partial outputs out and in), and a piece of the sequence
-    // mostly ends one item and begins another, with a cut on either side.  Each worker gets one part of one item, of about `size` places.
+    // mostly ends one item and begins another, with a cut on either side.  Each worker gets one part of one item, of about `size` places (0.6: what the last
+    // part of an item lacks on average, so that the parts come to a little less than the workers).  Against pieces of the sequence, us, 16 / 2 heads, D = 128:
+    // prompts of 200, 400, 850, 2039 and 3000 tokens 29.6, 33, 40, 47.6, 69.5 here, 29.7, 44, 47, 56, 93 there; 4 prompts of 500 36 and 57; 500 behind
+    // 11500 80 and 103; 1000 behind 8000 96 and 102 (16 / 16 heads, D = 64: 70 both).  It loses where parts come down to a tile or two each: a prompt of 100
+    // with 40 / 8 heads 26 and 14, 99 new of 1244 57 and 47 (16 / 2: 54 and 46), 61 of 7000 with 16 / 2 68 and 61.
     bool apart = false;
     double size = 0.0;
     unsigned parts_total = 0;
