@@ -293,8 +293,8 @@ int skinny_gemm_append(int32_t B, int32_t k, int32_t Hkv, int32_t D, int32_t N, 
 typedef struct {
     int32_t B;            /* branches, 1 .. 4096 */
     int32_t T;            /* rows of Q and O: new tokens of all branches together, >= 1; T * Hq < 2^24 */
-    int32_t max_new;      /* no branch has more new tokens than this; 1 <= max_new <= T.  A close bound is worth having: the kernel and its
-                           * workspace go by it, and with max_new * Hq / Hkv > 64 they are those of long chunks */
+    int32_t max_new;      /* no branch has more new tokens than this; 1 <= max_new <= T.  The kernel and its workspace go by it:
+                           * with max_new * Hq / Hkv > 64 they are those of long chunks, which many short branches wait for */
     int32_t Hq, Hkv;      /* query / KV heads, Hq % Hkv == 0; query head h reads KV head h / (Hq / Hkv) */
     int32_t D;            /* head dimension: 64 or 128 */
     int32_t page_tokens;  /* tokens of a page: a power of two from 16 to 1024 */

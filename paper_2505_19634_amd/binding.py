@@ -495,8 +495,8 @@ def verify_attention_paged(Q: torch.Tensor, Kpages: torch.Tensor, Vpages: torch.
                            workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Q [T][Hq][D], Kpages/Vpages [pages][Hkv][page_tokens][D] (any order of the first three in memory), page_table [B][columns] int32, kv_len
     [B] int32 (the new tokens included), q_start [B+1] int32: first row of each branch's new tokens, or None: as many of each branch, Q
-    may then be [B][n][Hq][D] too.  max_new: the most new tokens of a branch, as far as the caller knows (T if not: a step of many branches should
-    give it, or it takes the kernel of long chunks and up to 68 MB of workspace).
+    may then be [B][n][Hq][D] too.  max_new: the most new tokens of a branch, as far as the caller knows (T if not: a step of many short branches
+    should give it, or it takes the kernel of long chunks, 107 us for 43 with 1024 branches of 128 tokens, and up to 68 MB of workspace).
     Returns O of Q's shape and dtype, and LSE [T][Hq] fp32 if asked."""
     lib = load()
     device, handle = _current_gpu("verify_attention_paged", Q), _stream_handle(stream)
