@@ -67,3 +67,18 @@ def test_a_page_of_nothing_but_nan(lotts):
         blind = torch.zeros(48, dtype=torch.bool)
         blind[0:2] = blind[5:15] = True
         assert (out[blind] == 0).all() and torch.isnan(out[~blind]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_branches(lotts, D):
+    """More items than twice the units, every second branch with an infinity in its last new token's V: the tokens in front of it are as without."""
+    B, n = 300, 3
+    c = Cache([n] * B, [n + (b * 37) % 90 for b in range(B)], 8, 2, D, 16, seed=D)
+    clean = lotts.verify_attention_paged(c.Q, c.K, c.V, c.table, c.kv_len, c.q_start, max_new=n).view(B, n, 8, D)
+    last = c.kv_len.long() - 1
+    at = c.table[torch.arange(B, device=DEV), last // 16].long()
+    c.V[at[::2], 1, last[::2] % 16, 5] = math.inf
+    out = lotts.verify_attention_paged(c.Q, c.K, c.V, c.table, c.kv_len, c.q_start, max_new=n).view(B, n, 8, D)
+    off = torch.zeros(out.shape, dtype=torch.bool, device=DEV)
+    off[::2, n - 1, 4:, 5] = True
+    assert not torch.isfinite(out[off]).any() and torch.equal(out[~off], clean[~off])
