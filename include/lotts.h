@@ -425,6 +425,73 @@ int kv_pages_copy(void *pool, int32_t planes, int32_t pages, int64_t plane_strid
                   int32_t n, const int32_t *count, void *stream);
 
 /*
+ * Microscaled numbers.  32 neighbouring values of a row form a block: elements of few bits, and one power of two that they are multiples of.
+ *   MXFP4: elements e2m1, 4 bits, 0 0.5 1 1.5 2 3 4 6 and their negatives; two in a byte, the one with the lower index in the lower half
+ *   MXFP8: elements e4m3, 8 bits (the finite form: largest 448, no infinities, 0x7f and 0xff NaN)
+ *   scales: a byte s for each block (E8M0), 2^(s - 127)
+ * The calls that quantise choose the smallest power of two with which no value of the block lies behind the largest element, within s = 2 .. 252 (MXFP4) and
+ * 10 .. 246 (MXFP8), where everything that a block stands for is a normal bf16 or zero; every element is the nearest to its value, ties to the even one, and
+ * keeps its sign.  (Values beyond 1.5 * 2^127, MXFP4, and 1.75 * 2^127, MXFP8, become these.)  A block with an infinity or a NaN gets s = 255 and is NaN throughout.
+ * The calls that read take any bytes: s = 255 makes a block NaN; where an element times its power of two is no bf16 it is rounded to one.
+ */
+
+/*
+ * mxfp4_quantize -- a weight matrix to MXFP4, once, when it is loaded (Section 3.1: the step is bound by loading the weights; in this form
+ * they are 4.25 bits each).  mxfp4_dequantize -- the values that such a matrix stands for, exact in both types.
+ *   W, values [N][K] dtype (LOTTS_BF16 or LOTTS_F32; row pitch ldw, ld elements), codes [N][K / 2] bytes (ld_codes), scales [N][K / 32] bytes (ld_scales)
+ *   K a multiple of 32; N * K < 2^34; W, values and codes 16-byte aligned, their pitches multiples of 16 bytes
+ */
+int mxfp4_quantize(int32_t N, int32_t K, lotts_dtype dtype, const void *W, int64_t ldw, void *codes, int64_t ld_codes, void *scales,
+                   int64_t ld_scales, void *stream);
+int mxfp4_dequantize(int32_t N, int32_t K, lotts_dtype dtype, const void *codes, int64_t ld_codes, const void *scales, int64_t ld_scales,
+                     void *values, int64_t ld, void *stream);
+
+/* Bytes of workspace skinny_gemm_mxfp4 needs (0 if the sizes are invalid); never fewer for more tokens of the same matrix. */
+size_t skinny_gemm_mxfp4_workspace_bytes(int32_t M, int32_t N, int32_t K);
+
+/*
+ * skinny_gemm_mxfp4 -- skinny_gemm against a weight matrix in MXFP4: Y[m][n] = sum_k X[m][k] * W[n][k], W what codes and scales stand for.
+ *   X [M][K] bf16 (row pitch ldx elements), codes [N][K / 2] (ld_codes bytes), scales [N][K / 32] (ld_scales bytes), Y [M][N] bf16 out (ldy elements)
+ *   1 <= M <= 256; any N; K a multiple of 32 (both up to 2^26); X, codes, workspace 16-byte aligned, ldx a multiple of 8, ld_codes of 16; Y and scales as they are
+ * The weights become bf16, exactly, and the products accumulate in fp32 on the matrix cores, in an order that the sizes decide: the same data give the same bits.
+ *   workspace: >= skinny_gemm_mxfp4_workspace_bytes(M, N, K), any contents
+ */
+int skinny_gemm_mxfp4(int32_t M, int32_t N, int32_t K, const void *X, int64_t ldx, const void *codes, int64_t ld_codes, const void *scales,
+                      int64_t ld_scales, void *Y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * kv_append_paged_mxfp8 -- kv_append_paged into a cache in MXFP8: the new tokens' K and V rows are quantised as they are written.
+ *   Knew, Vnew [T][Hkv][D] dtype (LOTTS_BF16 or LOTTS_F32) views, page_table, kv_len, q_start: as for kv_append_paged; D a multiple of 32
+ *   Kpages, Vpages: [pages][Hkv][page_tokens][D] bytes in/out (strides in bytes, multiples of 16; 16-byte aligned)
+ *   Kscales, Vscales: [pages][Hkv][page_tokens][D / 32] bytes in/out (strides in bytes; the two share them)
+ * A token that kv_append_paged skips is skipped here; nothing else in pages and scales is touched.
+ */
+int kv_append_paged_mxfp8(int32_t B, int32_t T, int32_t Hkv, int32_t D, int32_t page_tokens, int32_t pages, int32_t columns, lotts_dtype dtype,
+                          const void *Knew, const void *Vnew, int64_t new_stride_t, int64_t new_stride_h, void *Kpages, void *Vpages,
+                          int64_t page_stride_p, int64_t page_stride_h, int64_t page_stride_t, void *Kscales, void *Vscales, int64_t scale_stride_p,
+                          int64_t scale_stride_h, int64_t scale_stride_t, const int32_t *page_table, int64_t table_stride, const int32_t *kv_len,
+                          const int32_t *q_start, void *stream);
+
+/* Geometry of one verify_attention_paged_mxfp8 call.  paged: as for verify_attention_paged, with dtype that of Q and O and the page strides in bytes. */
+typedef struct {
+    lotts_paged_desc paged;
+    int64_t scale_stride_p, scale_stride_h, scale_stride_t;   /* Kscales, Vscales [pages][Hkv][page_tokens][D / 32], bytes; 0: dense */
+} lotts_paged_mx_desc;
+
+/* As verify_attention_paged_workspace_bytes. */
+size_t verify_attention_paged_mxfp8_workspace_bytes(const lotts_paged_mx_desc *desc);
+
+/*
+ * verify_attention_paged_mxfp8 -- verify_attention_paged over a cache in MXFP8, as kv_append_paged_mxfp8 writes it: half of the bytes to read.
+ *   Kpages, Vpages [pages][Hkv][page_tokens][D] bytes, 16-byte aligned; Kscales, Vscales [pages][Hkv][page_tokens][D / 32] bytes
+ *   the other arguments, the workspace (zero-filled once, then this entry point's own) and what holds for all of them: as for verify_attention_paged
+ * The cached values are exact in bf16 and are multiplied as such (bf16 Q) or as fp32 (fp32 Q).  A NaN in V reaches the rows that see its key and no others.
+ */
+int verify_attention_paged_mxfp8(const lotts_paged_mx_desc *desc, const void *Q, const void *Kpages, const void *Vpages, const void *Kscales,
+                                 const void *Vscales, const int32_t *page_table, const int32_t *kv_len, const int32_t *q_start, void *O, float *lse,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Kernel timer -- device execution time of the kernels the entry points launch, for callers that
  * have no profiler at hand (not an operation of the paper; a measurement aid).
  * Between lotts_timer_start and lotts_timer_stop every kernel launched by the CALLING HOST THREAD
@@ -443,7 +510,8 @@ int kv_pages_copy(void *pool, int32_t planes, int32_t pages, int64_t plane_strid
  * spec_accept 1 (2 -- scan, pick -- when V is beyond 2^18); spec_accept_logits 2 (row statistics, scan and
  * pick); majority_vote 1; confidence_vote 1; skinny_gemm 1 (2 when K is split: GEMM, reduce),
  * skinny_gemm_append the same (and kv_append where a product that streams W has K unsplit); verify_attention_paged 1; kv_append_paged 1;
- * kv_pages_reserve, _fork, _free, _copy 1; kv_pages_compact 2.
+ * kv_pages_reserve, _fork, _free, _copy 1; kv_pages_compact 2; mxfp4_quantize, mxfp4_dequantize, kv_append_paged_mxfp8,
+ * verify_attention_paged_mxfp8 1; skinny_gemm_mxfp4 1.
  */
 int lotts_timer_start(int32_t max_launches);
 int lotts_timer_pause(int32_t paused);

@@ -1,5 +1,5 @@
 """Thin Python binding of liblotts.so: argument marshalling only.  The calls that are shorter on the GPU than in Python
-(verify_attention, verify_attention_noalloc, spec_accept, majority_vote, skinny_gemm, the paged cache's) go through the extension _calls, the
+(verify_attention, verify_attention_noalloc, spec_accept, majority_vote, skinny_gemm, the paged cache's, the microscaled ones) go through the extension _calls, the
 others through ctypes.
 
 torch supplies device memory and the current stream; every step of the verify path runs in
@@ -24,6 +24,8 @@ EXPORTS = ("lotts_strerror", "verify_attention_workspace_bytes", "verify_attenti
            "majority_vote", "confidence_vote", "skinny_gemm_workspace_bytes", "skinny_gemm", "skinny_gemm_append", "kv_append",
            "greedy_search", "verify_attention_paged_workspace_bytes", "verify_attention_paged", "kv_append_paged", "kv_pages_workspace_bytes",
            "kv_pages_reserve", "kv_pages_fork", "kv_pages_free", "kv_pages_compact", "kv_pages_copy",
+           "mxfp4_quantize", "mxfp4_dequantize", "skinny_gemm_mxfp4_workspace_bytes", "skinny_gemm_mxfp4", "kv_append_paged_mxfp8",
+           "verify_attention_paged_mxfp8_workspace_bytes", "verify_attention_paged_mxfp8",
            "lotts_timer_start", "lotts_timer_pause", "lotts_timer_stop")
 
 
@@ -45,6 +47,11 @@ class PagedDesc(ctypes.Structure):
                 [("scale", ctypes.c_float)] +
                 [(n, ctypes.c_int64) for n in ("q_stride_t", "q_stride_h", "page_stride_p", "page_stride_h", "page_stride_t", "table_stride",
                                                "o_stride_t", "o_stride_h")])
+
+
+class PagedMxDesc(ctypes.Structure):
+    """Mirror of lotts_paged_mx_desc."""
+    _fields_ = [("paged", PagedDesc)] + [(n, ctypes.c_int64) for n in ("scale_stride_p", "scale_stride_h", "scale_stride_t")]
 
 
 TTS_TASK_FN = ctypes.CFUNCTYPE(ctypes.c_double, ctypes.c_int32, ctypes.c_int32, ctypes.c_double, ctypes.c_void_p)
@@ -135,12 +142,29 @@ def load() -> ctypes.CDLL:
         lib.kv_pages_compact.argtypes = [i32] * 3 + [vp, i64, vp, vp, vp, vp, sz, vp]
         lib.kv_pages_copy.restype = ctypes.c_int
         lib.kv_pages_copy.argtypes = [vp, i32, i32, i64, i64, i64, vp, i32, vp, vp]
+        lib.mxfp4_quantize.restype = ctypes.c_int
+        lib.mxfp4_quantize.argtypes = [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp]
+        lib.mxfp4_dequantize.restype = ctypes.c_int
+        lib.mxfp4_dequantize.argtypes = [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp]
+        lib.skinny_gemm_mxfp4_workspace_bytes.restype = sz
+        lib.skinny_gemm_mxfp4_workspace_bytes.argtypes = [i32, i32, i32]
+        lib.skinny_gemm_mxfp4.restype = ctypes.c_int
+        lib.skinny_gemm_mxfp4.argtypes = [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+        lib.kv_append_paged_mxfp8.restype = ctypes.c_int
+        lib.kv_append_paged_mxfp8.argtypes = [i32] * 8 + [vp, vp, i64, i64] + [vp, vp, i64, i64, i64] * 2 + [vp, i64, vp, vp, vp]
+        lib.verify_attention_paged_mxfp8_workspace_bytes.restype = sz
+        lib.verify_attention_paged_mxfp8_workspace_bytes.argtypes = [ctypes.POINTER(PagedMxDesc)]
+        lib.verify_attention_paged_mxfp8.restype = ctypes.c_int
+        lib.verify_attention_paged_mxfp8.argtypes = [ctypes.POINTER(PagedMxDesc)] + [vp] * 10 + [vp, sz, vp]
         lib.calls = _calls.Calls(*(ctypes.cast(f, vp).value for f in (
             lib.verify_attention_workspace_bytes, lib.verify_attention, lib.spec_accept_workspace_bytes, lib.spec_accept,
             lib.majority_vote, lib.skinny_gemm_workspace_bytes, lib.skinny_gemm, lib.verify_attention_noalloc)))
         lib.paged = _calls.PagedCalls(*(ctypes.cast(f, vp).value for f in (
             lib.verify_attention_paged_workspace_bytes, lib.verify_attention_paged, lib.kv_append_paged, lib.kv_pages_reserve, lib.kv_pages_fork,
             lib.kv_pages_free, lib.kv_pages_compact, lib.kv_pages_copy)))
+        lib.mx = _calls.MxCalls(*(ctypes.cast(f, vp).value for f in (
+            lib.mxfp4_quantize, lib.mxfp4_dequantize, lib.skinny_gemm_mxfp4_workspace_bytes, lib.skinny_gemm_mxfp4, lib.kv_append_paged_mxfp8,
+            lib.verify_attention_paged_mxfp8_workspace_bytes, lib.verify_attention_paged_mxfp8)))
         _lib = lib
     return _lib
 
@@ -483,7 +507,7 @@ def kv_append(Knew: torch.Tensor, Vnew: torch.Tensor, Kpriv: torch.Tensor, Vpriv
 
 
 def _current_gpu(where: str, t: torch.Tensor) -> int:
-    """The current device's number; the paged calls' tensors all lie there."""
+    """The current device's number; the paged and the microscaled calls' tensors all lie there."""
     if not t.is_cuda:
         raise ValueError("%s runs on the GPU only" % where)
     return torch._C._cuda_getDevice()
@@ -587,6 +611,89 @@ def kv_pages_copy(pool: torch.Tensor, pairs: torch.Tensor, *, count: Optional[to
     rc = lib.paged.kv_pages_copy(pool, pairs, count, _current_gpu("kv_pages_copy", pool), _stream_handle(stream))
     if rc != 0:
         raise LottsError(rc, "kv_pages_copy")
+
+
+def mxfp4_quantize(W: torch.Tensor, *, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None):
+    """W [N][K] bfloat16 or float32 on the GPU, K a multiple of 32, rows may be strided, to MXFP4: returns (codes [N][K/2] uint8, the lower half of a byte
+    first, scales [N][K/32] float8_e8m0fnu)."""
+    lib = load()
+    device = _current_gpu("mxfp4_quantize", W)
+    if W.dim() != 2:
+        raise ValueError("the matrix must be [N][K] with contiguous rows")
+    if codes is None:
+        codes = torch.empty((W.shape[0], W.shape[1] // 2), dtype=torch.uint8, device=W.device)
+    if scales is None:
+        scales = torch.empty((W.shape[0], W.shape[1] // 32), dtype=torch.float8_e8m0fnu, device=W.device)
+    rc = lib.mx.mxfp4_quantize(W, codes, scales, device, _stream_handle(stream))
+    if rc != 0:
+        raise LottsError(rc, "mxfp4_quantize")
+    return codes, scales
+
+
+def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, *, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The values [N][K] that codes [N][K/2] uint8 and scales [N][K/32] (float8_e8m0fnu or uint8) stand for, exact in bfloat16 and float32."""
+    lib = load()
+    device = _current_gpu("mxfp4_dequantize", codes)
+    if codes.dim() != 2:
+        raise ValueError("codes must be [N][K / 2] with contiguous rows")
+    if out is None:
+        out = torch.empty((codes.shape[0], 2 * codes.shape[1]), dtype=dtype, device=codes.device)
+    rc = lib.mx.mxfp4_dequantize(out, codes, scales, device, _stream_handle(stream))
+    if rc != 0:
+        raise LottsError(rc, "mxfp4_dequantize")
+    return out
+
+
+def skinny_gemm_mxfp4(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Y = X @ W.T for bf16 X [M][K] (M <= 256) and the MXFP4 weights W [N][K] of codes [N][K/2] uint8 and scales [N][K/32] (float8_e8m0fnu or uint8), as
+    mxfp4_quantize makes them; rows may be strided."""
+    lib = load()
+    device, handle = _current_gpu("skinny_gemm_mxfp4", X), _stream_handle(stream)
+    if out is None:
+        if X.dim() != 2 or codes.dim() != 2:
+            raise ValueError("X must be [M][K] and codes [N][K / 2] with contiguous rows")
+        out = torch.empty((X.shape[0], codes.shape[0]), dtype=torch.bfloat16, device=X.device)
+    cached = None if workspace is not None else _workspaces.get(_workspace_key("gemm_mxfp4", device, stream))
+    call = lib.mx.skinny_gemm_mxfp4
+    rc = call(X, codes, scales, out, workspace, cached, device, handle)
+    if rc != 0:
+        _finish(rc, "gemm_mxfp4", device, stream, lambda ws: call(X, codes, scales, out, None, ws, device, handle), "skinny_gemm_mxfp4")
+    return out
+
+
+def kv_append_paged_mxfp8(Knew: torch.Tensor, Vnew: torch.Tensor, Kpages: torch.Tensor, Vpages: torch.Tensor, Kscales: torch.Tensor, Vscales: torch.Tensor,
+                          page_table: torch.Tensor, kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None, *,
+                          stream: Optional[torch.cuda.Stream] = None) -> None:
+    """kv_append_paged into a cache in MXFP8: Knew/Vnew [T][Hkv][D] bfloat16 or float32 are quantised as they are written to Kpages/Vpages
+    [pages][Hkv][page_tokens][D] (float8_e4m3fn or uint8) and Kscales/Vscales [pages][Hkv][page_tokens][D/32] (float8_e8m0fnu or uint8), in place."""
+    lib = load()
+    rc = lib.mx.kv_append_paged_mxfp8(Knew, Vnew, Kpages, Vpages, Kscales, Vscales, page_table, kv_len, q_start,
+                                      _current_gpu("kv_append_paged_mxfp8", Knew), _stream_handle(stream))
+    if rc != 0:
+        raise LottsError(rc, "kv_append_paged_mxfp8")
+
+
+def verify_attention_paged_mxfp8(Q: torch.Tensor, Kpages: torch.Tensor, Vpages: torch.Tensor, Kscales: torch.Tensor, Vscales: torch.Tensor,
+                                 page_table: torch.Tensor, kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None, *, max_new: Optional[int] = None,
+                                 scale: float = 0.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, return_lse: bool = False,
+                                 workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """verify_attention_paged over a cache in MXFP8 (as kv_append_paged_mxfp8 describes it); Q and O are bfloat16 or float32, the other arguments as there."""
+    lib = load()
+    device, handle = _current_gpu("verify_attention_paged_mxfp8", Q), _stream_handle(stream)
+    if out is None:
+        out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if return_lse and lse is None:
+        lse = torch.empty((Q.numel() // max(1, Q.shape[-1] * Q.shape[-2]), Q.shape[-2]), dtype=torch.float32, device=Q.device)
+    cached = None if workspace is not None else _workspaces.get(_workspace_key("attn_paged_mxfp8", device, stream))
+    call = lib.mx.verify_attention_paged_mxfp8
+    args = (Q, Kpages, Vpages, Kscales, Vscales, page_table, kv_len, q_start, max_new, scale, out, lse)
+    rc = call(*args, workspace, cached, device, handle)
+    if rc != 0:
+        _finish(rc, "attn_paged_mxfp8", device, stream, lambda ws: call(*args, None, ws, device, handle), "verify_attention_paged_mxfp8")
+    return (out, lse) if return_lse else out
 
 
 class kernel_timer:

@@ -15,7 +15,8 @@ CALIB = os.path.join(_HERE, "calib_copy")
 PROBE = os.path.join(_HERE, "libread_probe.so")
 CALLS = os.path.join(_HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["verify_attention.hip", "spec_accept.hip", "spec_accept_logits.hip", "majority_vote.hip",
-           "confidence_vote.hip", "skinny_gemm.hip", "kv_append.hip", "paged_attention.hip", "kv_pages.hip", "kernel_timer.hip", "greedy_search.cpp"]
+           "confidence_vote.hip", "skinny_gemm.hip", "kv_append.hip", "paged_attention.hip", "kv_pages.hip", "mxfp4.hip",
+           "skinny_gemm_mxfp4.hip", "kernel_timer.hip", "greedy_search.cpp"]
 
 
 FLAGS = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -1,5 +1,5 @@
 // The host side of the calls that are shorter on the GPU than in Python: argument checks, the descriptor and the library call of
-// verify_attention (and its _noalloc form), spec_accept, majority_vote and skinny_gemm, and of the paged cache's calls, as a CPython extension on torch's tensors.  binding.py keeps
+// verify_attention (and its _noalloc form), spec_accept, majority_vote and skinny_gemm, and of the paged cache's and the microscaled calls, as a CPython extension on torch's tensors.  binding.py keeps
 // the signatures, makes what a caller leaves out and holds the workspaces; a call that finds its workspace missing or too small
 // says how much it needs and is made again.
 // Measured (2 branches, fp32, vocabulary 1000): a step's three calls through ctypes are 6.5 + 6.5 + 4.1 us of host time for
@@ -404,6 +404,47 @@ Tokens tokens_of(const at::Tensor& t, int64_t B, bool uniform) {
 }
 int64_t pitch(int64_t n, int64_t stride, int64_t dense) { return n > 1 ? stride : std::max(stride, dense); }
 
+// What verify_attention_paged and verify_attention_paged_mxfp8 share: the rows of Q and out, lengths, first rows, lse, and the numbers of the call.
+struct Rows {
+    Tokens q, o;
+    const int32_t *lens, *start;
+    int32_t most, dtype;
+    float scale;
+    float* lse;
+};
+Rows rows_of_call(const OneDevice& on, const at::Tensor& Q, const at::Tensor& O, const at::Tensor& K, const Table& tab, const at::Tensor& len, PyObject* q_start, bool uniform,
+                  PyObject* max_new, PyObject* softmax_scale, PyObject* lse) {
+    Rows r;
+    r.q = tokens_of(Q, tab.B, uniform), r.o = tokens_of(O, tab.B, uniform);
+    if (O.sizes() != Q.sizes()) throw Error{PyExc_ValueError, "out must have Q's shape"};
+    if (O.scalar_type() != Q.scalar_type()) throw Error{PyExc_TypeError, "Q and out share one dtype"};
+    if (K.size(3) != r.q.D) throw Error{PyExc_ValueError, "Q and Kpages disagree"};
+    if (r.q.T > 0x7fffffff) throw Error{PyExc_ValueError, "too many tokens"};
+    r.lens = numbers(len, tab.B, "kv_len must be contiguous int32 [B]");
+    r.start = uniform ? nullptr : numbers(on(q_start, "q_start must be a tensor"), (int64_t)tab.B + 1, "q_start must be contiguous int32 [B+1]");
+    long most = max_new == Py_None ? (uniform ? std::max<long>(1, r.q.T / std::max(1, tab.B)) : (long)r.q.T) : PyLong_AsLong(max_new);
+    const double scale = PyFloat_AsDouble(softmax_scale);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Error{PyExc_TypeError, "max_new and scale must be numbers"};
+    }
+    if (scale != 0.0 && (float)scale == 0.0f) throw Error{PyExc_ValueError, "the scale is nothing in float32"};  // (where 0 selects 1 / sqrt(D))
+    if (most < 0 || most > 0x7fffffff) most = 0;
+    if (uniform && most * tab.B != r.q.T) throw Error{PyExc_ValueError, "without q_start every branch has T / B new tokens"};
+    r.most = (int32_t)most, r.scale = (float)scale, r.dtype = paged_dtype(Q);
+    r.lse = nullptr;
+    if (lse != Py_None) {
+        on(lse, "lse must be a tensor");
+        r.lse = rows_of<float>(lse, at::kFloat, r.q.T * r.q.H, "lse must be contiguous float32 [T][Hq]");
+    }
+    return r;
+}
+lotts_paged_desc paged_geometry(const Rows& r, const at::Tensor& K, const Table& tab) {
+    return {tab.B, (int32_t)r.q.T, r.most, (int32_t)r.q.H, (int32_t)K.size(1), (int32_t)r.q.D, (int32_t)K.size(2), (int32_t)K.size(0), tab.columns,
+            r.dtype, r.scale, pitch(r.q.T, r.q.stride_t, r.q.H * r.q.D), pitch(r.q.H, r.q.stride_h, r.q.D), K.stride(0), K.stride(1),
+            pitch(K.size(2), K.stride(2), r.q.D), tab.stride, pitch(r.o.T, r.o.stride_t, r.q.H * r.q.D), pitch(r.o.H, r.o.stride_h, r.q.D)};
+}
+
 // Q, Kpages, Vpages, page_table, kv_len, q_start, max_new, scale, out, lse, workspace, cached workspace, device, stream
 PyObject* call_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     const PagedCalls* c = reinterpret_cast<PagedCalls*>(self);
@@ -415,30 +456,9 @@ PyObject* call_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         const bool uniform = a[5] == Py_None;
         const Table tab = table_of(table);
         same_pages(K, V);
-        const Tokens q = tokens_of(Q, tab.B, uniform), o = tokens_of(O, tab.B, uniform);
-        if (O.sizes() != Q.sizes()) throw Error{PyExc_ValueError, "out must have Q's shape"};
-        if (K.scalar_type() != Q.scalar_type() || O.scalar_type() != Q.scalar_type()) throw Error{PyExc_TypeError, "Q, K, V and out share one dtype"};
-        if (K.size(3) != q.D) throw Error{PyExc_ValueError, "Q and Kpages disagree"};
-        if (q.T > 0x7fffffff) throw Error{PyExc_ValueError, "too many tokens"};
-        const int32_t* lens = numbers(len, tab.B, "kv_len must be contiguous int32 [B]");
-        const int32_t* start = uniform ? nullptr : numbers(on(a[5], "q_start must be a tensor"), (int64_t)tab.B + 1, "q_start must be contiguous int32 [B+1]");
-        long most = a[6] == Py_None ? (uniform ? std::max<long>(1, q.T / std::max(1, tab.B)) : (long)q.T) : PyLong_AsLong(a[6]);
-        const double scale = PyFloat_AsDouble(a[7]);
-        if (PyErr_Occurred()) {
-            PyErr_Clear();
-            throw Error{PyExc_TypeError, "max_new and scale must be numbers"};
-        }
-        if (scale != 0.0 && (float)scale == 0.0f) throw Error{PyExc_ValueError, "the scale is nothing in float32"};  // (where 0 selects 1 / sqrt(D))
-        if (most < 0 || most > 0x7fffffff) most = 0;
-        if (uniform && most * tab.B != q.T) throw Error{PyExc_ValueError, "without q_start every branch has T / B new tokens"};
-        float* lse = nullptr;
-        if (a[9] != Py_None) {
-            on(a[9], "lse must be a tensor");
-            lse = rows_of<float>(a[9], at::kFloat, q.T * q.H, "lse must be contiguous float32 [T][Hq]");
-        }
-        lotts_paged_desc d = {tab.B, (int32_t)q.T, (int32_t)most, (int32_t)q.H, (int32_t)K.size(1), (int32_t)q.D, (int32_t)K.size(2), (int32_t)K.size(0), tab.columns,
-                              paged_dtype(Q), (float)scale, pitch(q.T, q.stride_t, q.H * q.D), pitch(q.H, q.stride_h, q.D), K.stride(0), K.stride(1),
-                              pitch(K.size(2), K.stride(2), q.D), tab.stride, pitch(o.T, o.stride_t, q.H * q.D), pitch(o.H, o.stride_h, q.D)};
+        if (K.scalar_type() != Q.scalar_type()) throw Error{PyExc_TypeError, "Q, K, V and out share one dtype"};
+        const Rows r = rows_of_call(on, Q, O, K, tab, len, a[5], uniform, a[6], a[7], a[9]);
+        const lotts_paged_desc d = paged_geometry(r, K, tab);
         const size_t need = c->attn_ws(&d);
         if (need == 0) return kNoWorkspaceQuery;
         void* ws;
@@ -447,7 +467,7 @@ PyObject* call_paged(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         if (!workspace(a[10], a[11], need, &ws, &bytes)) return (Py_ssize_t)need;
         const void *qp = Q.data_ptr(), *kp = K.data_ptr(), *vp = V.data_ptr();
         void *op = O.data_ptr(), *stream = address(a[13]);
-        return released([&] { return c->attn(&d, qp, kp, vp, tab.entries, lens, start, op, lse, ws, bytes, stream); });
+        return released([&] { return c->attn(&d, qp, kp, vp, tab.entries, r.lens, r.start, op, r.lse, ws, bytes, stream); });
     });
 }
 
@@ -631,6 +651,220 @@ PyMethodDef paged_methods[] = {
 
 PyTypeObject paged_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
+// ---- microscaled numbers -------------------------------------------------------------------------------------------------
+using quantize_fn = decltype(&mxfp4_quantize);
+using dequantize_fn = decltype(&mxfp4_dequantize);
+using gemm4_ws_fn = decltype(&skinny_gemm_mxfp4_workspace_bytes);
+using gemm4_fn = decltype(&skinny_gemm_mxfp4);
+using append8_fn = decltype(&kv_append_paged_mxfp8);
+using paged8_ws_fn = decltype(&verify_attention_paged_mxfp8_workspace_bytes);
+using paged8_fn = decltype(&verify_attention_paged_mxfp8);
+
+struct MxCalls {
+    PyObject_HEAD
+    quantize_fn quantize;
+    dequantize_fn dequantize;
+    gemm4_ws_fn gemm_ws;
+    gemm4_fn gemm;
+    append8_fn append;
+    paged8_ws_fn attn_ws;
+    paged8_fn attn;
+};
+
+constexpr int64_t kBlock = 32;  // values that share a scale
+
+void scale_type(const at::Tensor& t) {
+    if (t.scalar_type() != at::kByte && t.scalar_type() != at::kFloat8_e8m0fnu) throw Error{PyExc_TypeError, "scales must be float8_e8m0fnu or uint8"};
+}
+// Rows that lie apart, the elements of a row next to each other.
+void dense_rows(const at::Tensor& t, const char* what) {
+    if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) throw Error{PyExc_ValueError, what};
+    if (expanded(t)) throw Error{PyExc_ValueError, "expanded tensors are not supported"};
+}
+struct Matrix4 {  // codes and scales of [N][K]
+    int64_t N, K, ld_codes, ld_scales;
+    void *codes, *scales;
+};
+Matrix4 matrix4(const OneDevice& on, PyObject* c, PyObject* s) {
+    const at::Tensor &codes = on(c, "codes must be a tensor"), &scales = on(s, "scales must be a tensor");
+    dense_rows(codes, "codes must be [N][K / 2] with contiguous rows");
+    dense_rows(scales, "scales must be [N][K / 32] with contiguous rows");
+    if (codes.scalar_type() != at::kByte) throw Error{PyExc_TypeError, "codes must be uint8"};
+    scale_type(scales);
+    const int64_t N = codes.size(0), K = 2 * codes.size(1);
+    if (scales.size(0) != N || scales.size(1) * kBlock != K) throw Error{PyExc_ValueError, "codes [N][K / 2] and scales [N][K / 32] disagree"};
+    if (N > 0x7fffffff || K > 0x7fffffff) throw Error{PyExc_ValueError, "the matrix is too large"};
+    return {N, K, pitch(N, codes.stride(0), K / 2), pitch(N, scales.stride(0), K / kBlock), codes.data_ptr(), scales.data_ptr()};
+}
+
+// values, codes, scales, device, stream: mxfp4_quantize reads the first, mxfp4_dequantize writes it
+template <typename F>
+PyObject* convert4(PyObject* const* a, Py_ssize_t n, F call) {
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 5);
+        const OneDevice on{device_of(a[3])};
+        const at::Tensor& W = on(a[0], "the matrix must be a tensor");
+        dense_rows(W, "the matrix must be [N][K] with contiguous rows");
+        if (W.scalar_type() != at::kBFloat16 && W.scalar_type() != at::kFloat) throw Error{PyExc_TypeError, "the matrix must be bfloat16 or float32"};
+        const Matrix4 m = matrix4(on, a[1], a[2]);
+        if (W.size(0) != m.N || W.size(1) != m.K) throw Error{PyExc_ValueError, "the matrix [N][K] and codes [N][K / 2] disagree"};
+        void *values = W.data_ptr(), *stream = address(a[4]);
+        const int64_t ld = pitch(m.N, W.stride(0), m.K);
+        const lotts_dtype type = W.scalar_type() == at::kBFloat16 ? LOTTS_BF16 : LOTTS_F32;
+        return released([&] { return call(m, type, values, ld, stream); });
+    });
+}
+PyObject* call_quantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const MxCalls* c = reinterpret_cast<MxCalls*>(self);
+    return convert4(a, n, [c](const Matrix4& m, lotts_dtype type, void* values, int64_t ld, void* stream) {
+        return c->quantize((int32_t)m.N, (int32_t)m.K, type, values, ld, m.codes, m.ld_codes, m.scales, m.ld_scales, stream);
+    });
+}
+PyObject* call_dequantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const MxCalls* c = reinterpret_cast<MxCalls*>(self);
+    return convert4(a, n, [c](const Matrix4& m, lotts_dtype type, void* values, int64_t ld, void* stream) {
+        return c->dequantize((int32_t)m.N, (int32_t)m.K, type, m.codes, m.ld_codes, m.scales, m.ld_scales, values, ld, stream);
+    });
+}
+
+// X, codes, scales, out, workspace, cached workspace, device, stream
+PyObject* call_gemm4(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const MxCalls* c = reinterpret_cast<MxCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 8);
+        const OneDevice on{device_of(a[6])};
+        const at::Tensor &X = on(a[0], "X must be a tensor"), &Y = on(a[3], "out must be a tensor");
+        dense_rows(X, "X must be [M][K] with contiguous rows");
+        dense_rows(Y, "out must be [M][N] with contiguous rows");
+        if (X.scalar_type() != at::kBFloat16 || Y.scalar_type() != at::kBFloat16) throw Error{PyExc_TypeError, "X and out must be bfloat16"};
+        const Matrix4 w = matrix4(on, a[1], a[2]);
+        const int64_t M = X.size(0);
+        if (X.size(1) != w.K) throw Error{PyExc_ValueError, "X [M][K] and codes [N][K / 2] disagree"};
+        if (Y.size(0) != M || Y.size(1) != w.N) throw Error{PyExc_ValueError, "out must be [M][N]"};
+        if (M > 0x7fffffff) throw Error{PyExc_ValueError, "too many tokens"};
+        const size_t need = c->gemm_ws((int32_t)M, (int32_t)w.N, (int32_t)w.K);
+        if (need == 0) return kNoWorkspaceQuery;
+        void* ws;
+        size_t bytes;
+        if (a[4] != Py_None) on(a[4], "the workspace must be a tensor");
+        if (!workspace(a[4], a[5], need, &ws, &bytes)) return (Py_ssize_t)need;
+        const void* x = X.data_ptr();
+        void *y = Y.data_ptr(), *stream = address(a[7]);
+        const int64_t ldx = pitch(M, X.stride(0), w.K), ldy = pitch(M, Y.stride(0), w.N);
+        return released([&] { return c->gemm((int32_t)M, (int32_t)w.N, (int32_t)w.K, x, ldx, w.codes, w.ld_codes, w.scales, w.ld_scales, y, ldy, ws, bytes, stream); });
+    });
+}
+
+struct Scales {
+    void *K, *V;
+    int64_t p, h, t;
+};
+Scales scales_of(const at::Tensor& K, const at::Tensor& V, const at::Tensor& Ks, const at::Tensor& Vs) {
+    same_pages(K, V);
+    if (K.scalar_type() != at::kByte && K.scalar_type() != at::kFloat8_e4m3fn) throw Error{PyExc_TypeError, "Kpages and Vpages must be float8_e4m3fn or uint8"};
+    if (Ks.dim() != 4 || Vs.sizes() != Ks.sizes() || Vs.strides() != Ks.strides() || Ks.size(0) != K.size(0) || Ks.size(1) != K.size(1) || Ks.size(2) != K.size(2) ||
+        Ks.size(3) * kBlock != K.size(3))
+        throw Error{PyExc_ValueError, "Kscales and Vscales must be [pages][Hkv][page_tokens][D / 32] with shared strides"};
+    scale_type(Ks);
+    if (Vs.scalar_type() != Ks.scalar_type()) throw Error{PyExc_TypeError, "Kscales and Vscales share one dtype"};
+    if (Ks.size(3) > 1 && Ks.stride(3) != 1) throw Error{PyExc_ValueError, "the scales of a row must be contiguous"};
+    if (expanded(Ks)) throw Error{PyExc_ValueError, "expanded tensors are not supported"};
+    return {Ks.data_ptr(), Vs.data_ptr(), Ks.stride(0), Ks.stride(1), pitch(Ks.size(2), Ks.stride(2), Ks.size(3))};
+}
+
+// Q, Kpages, Vpages, Kscales, Vscales, page_table, kv_len, q_start, max_new, scale, out, lse, workspace, cached workspace, device, stream
+PyObject* call_paged8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const MxCalls* c = reinterpret_cast<MxCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 16);
+        const OneDevice on{device_of(a[14])};
+        const at::Tensor &Q = on(a[0], "Q must be a tensor"), &K = on(a[1], "Kpages must be a tensor"), &V = on(a[2], "Vpages must be a tensor"),
+                         &Ks = on(a[3], "Kscales must be a tensor"), &Vs = on(a[4], "Vscales must be a tensor"), &table = on(a[5], "page_table must be a tensor"),
+                         &len = on(a[6], "kv_len must be a tensor"), &O = on(a[10], "out must be a tensor");
+        const bool uniform = a[7] == Py_None;
+        const Table tab = table_of(table);
+        const Scales sc = scales_of(K, V, Ks, Vs);
+        const Rows r = rows_of_call(on, Q, O, K, tab, len, a[7], uniform, a[8], a[9], a[11]);
+        lotts_paged_mx_desc d = {paged_geometry(r, K, tab), sc.p, sc.h, sc.t};
+        const size_t need = c->attn_ws(&d);
+        if (need == 0) return kNoWorkspaceQuery;
+        void* ws;
+        size_t bytes;
+        if (a[12] != Py_None) on(a[12], "the workspace must be a tensor");
+        if (!workspace(a[12], a[13], need, &ws, &bytes)) return (Py_ssize_t)need;
+        const void *qp = Q.data_ptr(), *kp = K.data_ptr(), *vp = V.data_ptr();
+        void *op = O.data_ptr(), *stream = address(a[15]);
+        return released([&] { return c->attn(&d, qp, kp, vp, sc.K, sc.V, tab.entries, r.lens, r.start, op, r.lse, ws, bytes, stream); });
+    });
+}
+
+// Knew, Vnew, Kpages, Vpages, Kscales, Vscales, page_table, kv_len, q_start, device, stream
+PyObject* call_append8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    const MxCalls* c = reinterpret_cast<MxCalls*>(self);
+    return guarded([&]() -> Py_ssize_t {
+        expect(n, 11);
+        const OneDevice on{device_of(a[9])};
+        const at::Tensor &Kn = on(a[0], "Knew must be a tensor"), &Vn = on(a[1], "Vnew must be a tensor"), &K = on(a[2], "Kpages must be a tensor"),
+                         &V = on(a[3], "Vpages must be a tensor"), &Ks = on(a[4], "Kscales must be a tensor"), &Vs = on(a[5], "Vscales must be a tensor"),
+                         &table = on(a[6], "page_table must be a tensor"), &len = on(a[7], "kv_len must be a tensor");
+        const bool uniform = a[8] == Py_None;
+        const Table tab = table_of(table);
+        const Scales sc = scales_of(K, V, Ks, Vs);
+        if (Vn.sizes() != Kn.sizes() || Vn.strides() != Kn.strides()) throw Error{PyExc_ValueError, "Knew and Vnew must share shape and strides"};
+        const Tokens k = tokens_of(Kn, tab.B, uniform);
+        const lotts_dtype dt = (lotts_dtype)paged_dtype(Kn);
+        if (Vn.scalar_type() != Kn.scalar_type()) throw Error{PyExc_TypeError, "Knew and Vnew share one dtype"};
+        if (K.size(1) != k.H || K.size(3) != k.D) throw Error{PyExc_ValueError, "Knew and Kpages disagree"};
+        if (k.T > 0x7fffffff) throw Error{PyExc_ValueError, "too many tokens"};
+        const int32_t* lens = numbers(len, tab.B, "kv_len must be contiguous int32 [B]");
+        const int32_t* start = uniform ? nullptr : numbers(on(a[8], "q_start must be a tensor"), (int64_t)tab.B + 1, "q_start must be contiguous int32 [B+1]");
+        const void *kn = Kn.data_ptr(), *vn = Vn.data_ptr();
+        void *kp = K.data_ptr(), *vp = V.data_ptr(), *stream = address(a[10]);
+        return released([&] {
+            return c->append(tab.B, (int32_t)k.T, (int32_t)k.H, (int32_t)k.D, (int32_t)K.size(2), (int32_t)K.size(0), tab.columns, dt, kn, vn, k.stride_t,
+                             pitch(k.H, k.stride_h, k.D), kp, vp, K.stride(0), K.stride(1), pitch(K.size(2), K.stride(2), k.D), sc.K, sc.V, sc.p, sc.h, sc.t,
+                             tab.entries, tab.stride, lens, start, stream);
+        });
+    });
+}
+
+// MxCalls(address of mxfp4_quantize, mxfp4_dequantize, skinny_gemm_mxfp4_workspace_bytes, skinny_gemm_mxfp4, kv_append_paged_mxfp8,
+// verify_attention_paged_mxfp8_workspace_bytes, verify_attention_paged_mxfp8)
+PyObject* mx_new(PyTypeObject* type, PyObject* args, PyObject*) {
+    void* f[7];
+    if (PyTuple_GET_SIZE(args) != 7) {
+        PyErr_SetString(PyExc_TypeError, "seven addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 7; ++i) {
+        f[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(args, i));
+        if (!f[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an address is 0");
+            return nullptr;
+        }
+    }
+    MxCalls* c = reinterpret_cast<MxCalls*>(type->tp_alloc(type, 0));
+    if (!c) return nullptr;
+    c->quantize = reinterpret_cast<quantize_fn>(f[0]);
+    c->dequantize = reinterpret_cast<dequantize_fn>(f[1]);
+    c->gemm_ws = reinterpret_cast<gemm4_ws_fn>(f[2]);
+    c->gemm = reinterpret_cast<gemm4_fn>(f[3]);
+    c->append = reinterpret_cast<append8_fn>(f[4]);
+    c->attn_ws = reinterpret_cast<paged8_ws_fn>(f[5]);
+    c->attn = reinterpret_cast<paged8_fn>(f[6]);
+    return reinterpret_cast<PyObject*>(c);
+}
+
+PyMethodDef mx_methods[] = {
+    {"mxfp4_quantize", (PyCFunction)(void (*)(void))call_quantize, METH_FASTCALL, nullptr},
+    {"mxfp4_dequantize", (PyCFunction)(void (*)(void))call_dequantize, METH_FASTCALL, nullptr},
+    {"skinny_gemm_mxfp4", (PyCFunction)(void (*)(void))call_gemm4, METH_FASTCALL, nullptr},
+    {"kv_append_paged_mxfp8", (PyCFunction)(void (*)(void))call_append8, METH_FASTCALL, nullptr},
+    {"verify_attention_paged_mxfp8", (PyCFunction)(void (*)(void))call_paged8, METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject mx_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
 PyMethodDef calls_methods[] = {
     {"verify_attention", (PyCFunction)(void (*)(void))call_attention, METH_FASTCALL, nullptr},
     {"verify_attention_noalloc", (PyCFunction)(void (*)(void))call_attention_noalloc, METH_FASTCALL, nullptr},
@@ -655,12 +889,17 @@ PyMODINIT_FUNC PyInit__calls(void) {
     paged_type.tp_flags = Py_TPFLAGS_DEFAULT;
     paged_type.tp_new = paged_new;
     paged_type.tp_methods = paged_methods;
-    if (PyType_Ready(&calls_type) < 0 || PyType_Ready(&paged_type) < 0) return nullptr;
+    mx_type.tp_name = "_calls.MxCalls";
+    mx_type.tp_basicsize = sizeof(MxCalls);
+    mx_type.tp_flags = Py_TPFLAGS_DEFAULT;
+    mx_type.tp_new = mx_new;
+    mx_type.tp_methods = mx_methods;
+    if (PyType_Ready(&calls_type) < 0 || PyType_Ready(&paged_type) < 0 || PyType_Ready(&mx_type) < 0) return nullptr;
     PyObject* m = PyModule_Create(&calls_module);
     if (!m) return nullptr;
-    for (PyTypeObject* type : {&calls_type, &paged_type}) {
+    for (PyTypeObject* type : {&calls_type, &paged_type, &mx_type}) {
         Py_INCREF(type);
-        if (PyModule_AddObject(m, type == &calls_type ? "Calls" : "PagedCalls", reinterpret_cast<PyObject*>(type)) < 0) {
+        if (PyModule_AddObject(m, type == &calls_type ? "Calls" : type == &paged_type ? "PagedCalls" : "MxCalls", reinterpret_cast<PyObject*>(type)) < 0) {
             Py_DECREF(type);
             Py_DECREF(m);
             return nullptr;

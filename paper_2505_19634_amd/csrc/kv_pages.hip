@@ -8,7 +8,7 @@
 // its threads.  References are counted with integer atomics, whose order changes nothing.
 #include <algorithm>
 
-#include "lotts_common.h"
+#include "mx.h"
 
 namespace lotts {
 
@@ -88,6 +88,62 @@ __global__ __launch_bounds__(256) void kv_append_paged_kernel(const AppendPagedP
                 *reinterpret_cast<p_u32x4*>(kd + to[j]) = k[j];
                 *reinterpret_cast<p_u32x4*>(vd + to[j]) = v[j];
             }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// kv_append_paged_mxfp8: the same, and the rows become 8-bit microscaled numbers (mx.h) on the way.  A lane has eight values of K and
+// of V at a time, four lanes a block.
+// ---------------------------------------------------------------------------------------------
+struct AppendPagedMxParams : AppendPagedParams {  // pieces: of eight values
+    unsigned char *Kscales, *Vscales;
+    long long scale_p, scale_h, scale_t;
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void kv_append_paged_mxfp8_kernel(const AppendPagedMxParams p) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave);
+    if (t >= p.T) return;
+    const unsigned char *ks = p.Knew + t * p.new_t, *vs = p.Vnew + t * p.new_t;
+    MxSource<T> k, v;
+    int h = 0, c = 0;
+    auto request = [&](int i) {
+        h = quot(i, p.d_pieces);
+        c = i - h * p.pieces;
+        if (i < p.n) {
+            k.load(ks + h * p.new_h + c * (int)(8 * sizeof(T)));
+            v.load(vs + h * p.new_h + c * (int)(8 * sizeof(T)));
+        }
+    };
+    request(lane);  // the source does not depend on where it goes
+    int b, pos;
+    if (p.q_start) {
+        b = branch_of(p.q_start, p.B, t, lane);
+        if (b >= p.B || t < p.q_start[b]) return;
+        pos = p.kv_len[b] - (p.q_start[b + 1] - t);
+    } else {
+        b = quot(t, p.d_r);
+        pos = p.kv_len[b] - ((b + 1) * p.R - t);
+    }
+    if (pos < 0 || pos >> p.shift >= p.columns) return;
+    const int page = p.table[b * p.table_stride + (pos >> p.shift)];
+    if (page < 0 || page >= p.pages) return;
+    const int row = pos & ((1 << p.shift) - 1);
+    const long long at = page * p.page_p + row * p.page_t, scale_at = page * p.scale_p + row * p.scale_t;
+    for (int i0 = 0; i0 < p.n; i0 += kWave) {
+        if (i0 > 0) request(i0 + lane);
+        if (i0 + lane < p.n) {  // (a row is whole blocks: four lanes leave or stay together)
+            auto put = [&](const MxSource<T>& src, unsigned char* codes, unsigned char* scales) {
+                float x[8];
+                src.values(x);
+                const unsigned s = mx_scale<E4M3>(mx_largest(x));
+                *reinterpret_cast<uint2*>(codes + at + h * p.page_h + c * 8) = mx_to_e4m3(x, s);
+                if ((c & 3) == 0) scales[scale_at + h * p.scale_h + (c >> 2)] = (unsigned char)s;
+            };
+            put(k, p.Kpages, p.Kscales);
+            put(v, p.Vpages, p.Vscales);
+        }
     }
 }
 
@@ -468,6 +524,48 @@ extern "C" int kv_append_paged(int32_t B, int32_t T, int32_t Hkv, int32_t D, int
     p.shift = shift; p.pages = pages; p.columns = columns;
     p.d_r = fast_div(q_start ? 1 : p.R); p.d_pieces = fast_div(p.pieces);
     LOTTS_LAUNCH(kv_append_paged_kernel, dim3((unsigned)((T + 3LL) / 4)), dim3(256), (hipStream_t)stream, p);
+    return check_launch();
+}
+
+extern "C" int kv_append_paged_mxfp8(int32_t B, int32_t T, int32_t Hkv, int32_t D, int32_t page_tokens, int32_t pages, int32_t columns,
+                                     lotts_dtype dtype, const void* Knew, const void* Vnew, int64_t new_stride_t, int64_t new_stride_h, void* Kpages,
+                                     void* Vpages, int64_t page_stride_p, int64_t page_stride_h, int64_t page_stride_t, void* Kscales, void* Vscales,
+                                     int64_t scale_stride_p, int64_t scale_stride_h, int64_t scale_stride_t, const int32_t* page_table,
+                                     int64_t table_stride, const int32_t* kv_len, const int32_t* q_start, void* stream) {
+    using namespace lotts;
+    if (dtype != LOTTS_BF16 && dtype != LOTTS_F32) return LOTTS_ERR_DTYPE;
+    const long long es = dtype == LOTTS_BF16 ? 2 : 4;
+    const int shift = page_shift(page_tokens);
+    if (B < 1 || B > kMaxBranches || T < 1 || T > (1 << 25) || Hkv < 1 || D < kMxBlock || D > 65536 || D % kMxBlock != 0 || shift < 0 || pages < 1 ||
+        pages > kMaxPages || columns < 1 || (long long)columns << shift > 0x7fffffffLL || table_stride < columns)
+        return LOTTS_ERR_SHAPE;
+    if (!Knew || !Vnew || !Kpages || !Vpages || !Kscales || !Vscales || !page_table || !kv_len) return LOTTS_ERR_NULL;
+    if (!q_start && T % B != 0) return LOTTS_ERR_SHAPE;
+    const int64_t from[2] = {new_stride_t, new_stride_h}, to[6] = {page_stride_p, page_stride_h, page_stride_t, scale_stride_p, scale_stride_h, scale_stride_t};
+    for (int64_t s : from)
+        if (s < 0 || (s * es) % 16 != 0) return LOTTS_ERR_SHAPE;
+    for (int i = 0; i < 6; ++i)
+        if (to[i] < 0 || (i < 3 && to[i] % 16 != 0)) return LOTTS_ERR_SHAPE;
+    if (new_stride_h < D || page_stride_t < D || scale_stride_t < D / kMxBlock || (long long)Hkv * D > (1 << 24)) return LOTTS_ERR_SHAPE;
+    if ((((uintptr_t)Knew | (uintptr_t)Vnew | (uintptr_t)Kpages | (uintptr_t)Vpages) & 15) != 0) return LOTTS_ERR_SHAPE;
+    AppendPagedMxParams p;
+    p.Knew = static_cast<const unsigned char*>(Knew);
+    p.Vnew = static_cast<const unsigned char*>(Vnew);
+    p.Kpages = static_cast<unsigned char*>(Kpages);
+    p.Vpages = static_cast<unsigned char*>(Vpages);
+    p.Kscales = static_cast<unsigned char*>(Kscales);
+    p.Vscales = static_cast<unsigned char*>(Vscales);
+    p.table = page_table; p.kv_len = kv_len; p.q_start = q_start;
+    p.new_t = new_stride_t * es; p.new_h = new_stride_h * es;
+    p.page_p = page_stride_p; p.page_h = page_stride_h; p.page_t = page_stride_t;
+    p.scale_p = scale_stride_p; p.scale_h = scale_stride_h; p.scale_t = scale_stride_t;
+    p.table_stride = table_stride;
+    p.B = B; p.T = T; p.R = T / B; p.Hkv = Hkv; p.pieces = D / 8; p.n = p.pieces * Hkv;
+    p.shift = shift; p.pages = pages; p.columns = columns;
+    p.d_r = fast_div(q_start ? 1 : p.R); p.d_pieces = fast_div(p.pieces);
+    const dim3 grid((unsigned)((T + 3LL) / 4));
+    if (dtype == LOTTS_BF16) LOTTS_LAUNCH(kv_append_paged_mxfp8_kernel<__bf16>, grid, dim3(256), (hipStream_t)stream, p);
+    else LOTTS_LAUNCH(kv_append_paged_mxfp8_kernel<float>, grid, dim3(256), (hipStream_t)stream, p);
     return check_launch();
 }
 

@@ -9,7 +9,7 @@
 #include <atomic>
 #include <cmath>
 
-#include "lotts_common.h"
+#include "mx.h"
 
 namespace lotts {
 
@@ -62,6 +62,12 @@ struct PagedParams {
     int part_rows;
     unsigned long long* cells;          // arrivals: [2][2 * workers], (call tag << 16) | arrivals
     unsigned long long tag;
+};
+
+// verify_attention_paged_mxfp8: K and V are codes, with their scales.
+struct PagedMxParams : PagedParams {
+    const unsigned char *Ks, *Vs;
+    long long scale_p, scale_h, scale_t;  // bytes
 };
 
 // A branch of the call: its first row of Q, its new tokens and all its tokens (both brought into the range that the arguments allow, so
@@ -1150,8 +1156,9 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) v
 // the states meet at the end.  The maximum is that of the scores as they are and the differences from it are scaled, so that the largest weight is 1
 // whatever the scale.
 // ---------------------------------------------------------------------------------------------
-template <int D, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedParams p) {
+template <int D, int WAVES, typename P, typename T>
+__global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const P p) {
+    constexpr bool MX = std::is_same<P, PagedMxParams>::value;
     constexpr int LPK = D / 4, KPL = kWave / LPK, NJ = 4, CHUNK = NJ * KPL;
     __shared__ __attribute__((aligned(16))) float sh_acc[WAVES][D];
     __shared__ float sh_ml[WAVES][2];
@@ -1176,22 +1183,37 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
     const int n = keys_of_row(branch_at(p, b), t);
     if (n < 0) return;
     const float scale = p.scale;
-    const float4 qv = *reinterpret_cast<const float4*>((const unsigned char*)p.Q + t * p.q_t + h * p.q_h + c4 * 16);
+    float4 qv;
+    {
+        const unsigned char* qp = (const unsigned char*)p.Q + t * p.q_t + h * p.q_h + c4 * (int)(4 * sizeof(T));
+        if constexpr (sizeof(T) == 2) {
+            const bf16x4 q4 = *reinterpret_cast<const bf16x4*>(qp);
+            qv = make_float4(q4[0], q4[1], q4[2], q4[3]);
+        } else {
+            qv = *reinterpret_cast<const float4*>(qp);
+        }
+    }
     const int32_t* row = p.table + b * p.table_stride;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float m = -INFINITY, l = 0.f;
     for (int j0 = wave * CHUNK; j0 < n; j0 += WAVES * CHUNK) {
         const int e = __builtin_amdgcn_readfirstlane(row[j0 >> p.shift]);
         if ((unsigned)e >= (unsigned)p.pages) continue;  // no page: nothing to see
-        const unsigned char* kp = (const unsigned char*)p.K + e * p.page_p + kvh * p.page_h + c4 * 16;
-        const unsigned char* vp = (const unsigned char*)p.V + e * p.page_p + kvh * p.page_h + c4 * 16;
+        const unsigned char* kp = (const unsigned char*)p.K + e * p.page_p + kvh * p.page_h + c4 * (MX ? 4 : 16);
+        const unsigned char* vp = (const unsigned char*)p.V + e * p.page_p + kvh * p.page_h + c4 * (MX ? 4 : 16);
         float4 kv[NJ], vv[NJ];
 #pragma unroll
         for (int i = 0; i < NJ; ++i) {
             const int j = min(j0 + i * KPL + grp, n - 1);  // keys behind the last one re-read it; masked below
             const long long off = (j & ((1 << p.shift) - 1)) * p.page_t;
-            kv[i] = *reinterpret_cast<const float4*>(kp + off);
-            vv[i] = *reinterpret_cast<const float4*>(vp + off);
+            if constexpr (MX) {
+                const long long scale_at = e * p.scale_p + kvh * p.scale_h + (j & ((1 << p.shift) - 1)) * p.scale_t + c4 / (kMxBlock / 4);
+                kv[i] = mx_f32_of_e4m3(*reinterpret_cast<const unsigned*>(kp + off), p.Ks[scale_at]);
+                vv[i] = mx_f32_of_e4m3(*reinterpret_cast<const unsigned*>(vp + off), p.Vs[scale_at]);
+            } else {
+                kv[i] = *reinterpret_cast<const float4*>(kp + off);
+                vv[i] = *reinterpret_cast<const float4*>(vp + off);
+            }
         }
         float s[NJ], mx = m;
 #pragma unroll
@@ -1242,7 +1264,7 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
             lsum += sh_ml[w][1] * wgt;
             o += sh_acc[w][tid] * wgt;
         }
-        reinterpret_cast<float*>((unsigned char*)p.O + t * p.o_t + h * p.o_h)[tid] = lsum == 0.f ? 0.f : o / lsum;
+        reinterpret_cast<T*>((unsigned char*)p.O + t * p.o_t + h * p.o_h)[tid] = (T)(lsum == 0.f ? 0.f : o / lsum);
         if (p.lse && tid == 0) p.lse[(long long)t * p.Hq + h] = M * scale + logf(lsum);
     }
 }
@@ -1250,7 +1272,7 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const PagedPar
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
-static int paged_desc(const lotts_paged_desc* in, bool uniform, lotts_paged_desc* d, int* shift) {
+static int paged_desc(const lotts_paged_desc* in, bool uniform, bool mx, lotts_paged_desc* d, int* shift) {
     if (!in) return LOTTS_ERR_NULL;
     *d = *in;
     if (d->dtype != LOTTS_F32 && d->dtype != LOTTS_BF16) return LOTTS_ERR_DTYPE;
@@ -1264,7 +1286,7 @@ static int paged_desc(const lotts_paged_desc* in, bool uniform, lotts_paged_desc
         if (d->page_tokens == 1 << s) *shift = s;
     if (*shift < 0 || (long long)d->columns << *shift > 0x3fffffffLL) return LOTTS_ERR_SHAPE;
     if (!(d->scale >= 0.0f) || d->scale > 3.0e38f) return LOTTS_ERR_SHAPE;
-    const long long D = d->D, es = d->dtype == LOTTS_BF16 ? 2 : 4;
+    const long long D = d->D, es = d->dtype == LOTTS_BF16 ? 2 : 4, cache_es = mx ? 1 : es;
     // 0 selects the dense layout
     if (!d->q_stride_h) d->q_stride_h = D;
     if (!d->q_stride_t) d->q_stride_t = d->Hq * D;
@@ -1274,11 +1296,13 @@ static int paged_desc(const lotts_paged_desc* in, bool uniform, lotts_paged_desc
     if (!d->page_stride_h) d->page_stride_h = d->page_tokens * D;
     if (!d->page_stride_p) d->page_stride_p = d->Hkv * d->page_tokens * D;
     if (!d->table_stride) d->table_stride = d->columns;
-    const long long st[] = {d->q_stride_t, d->q_stride_h, d->o_stride_t, d->o_stride_h, d->page_stride_p, d->page_stride_h, d->page_stride_t};
+    const long long st[] = {d->q_stride_t, d->q_stride_h, d->o_stride_t, d->o_stride_h}, page_st[] = {d->page_stride_p, d->page_stride_h, d->page_stride_t};
     for (long long s : st)
         if (s < 0 || (s * es) % 16 != 0) return LOTTS_ERR_SHAPE;
+    for (long long s : page_st)
+        if (s < 0 || (s * cache_es) % 16 != 0) return LOTTS_ERR_SHAPE;
     if (d->q_stride_h < D || d->o_stride_h < D || d->page_stride_t < D || d->table_stride < d->columns) return LOTTS_ERR_SHAPE;
-    if (d->page_stride_t * es > (1LL << 26)) return LOTTS_ERR_SHAPE;  // 16 keys of a page: 32-bit offsets
+    if (d->page_stride_t * cache_es > (1LL << 26)) return LOTTS_ERR_SHAPE;  // 16 keys of a page: 32-bit offsets
     // the sequence of work of a KV head in 32 bits (were every branch as long as the table allows)
     const long long G = d->Hq / d->Hkv, slots = (long long)d->T * G / kWideRows + d->B;
     if (((long long)d->columns << *shift) / kNarrowTile * kMaxWideCost + kMaxWideCost + kStartCost > 0x7fffffffLL / slots) return LOTTS_ERR_SHAPE;
@@ -1318,34 +1342,13 @@ static PagedPlan paged_plan(const lotts_paged_desc& d) {
     return pl;
 }
 
-}  // namespace lotts
-
-extern "C" size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc* desc) {
-    using namespace lotts;
-    lotts_paged_desc d;
-    int shift;
-    if (paged_desc(desc, false, &d, &shift) != LOTTS_OK) return 0;
-    return d.dtype == LOTTS_F32 ? 256 : paged_plan(d).bytes;
-}
-
-extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* Q, const void* Kpages, const void* Vpages, const int32_t* page_table,
-                                      const int32_t* kv_len, const int32_t* q_start, void* O, float* lse, void* workspace, size_t workspace_bytes,
-                                      void* stream) {
-    using namespace lotts;
-    lotts_paged_desc d;
-    int shift;
-    const int rc = paged_desc(desc, !q_start, &d, &shift);
-    if (rc != LOTTS_OK) return rc;
-    if (!Q || !Kpages || !Vpages || !page_table || !kv_len || !O || !workspace) return LOTTS_ERR_NULL;
-    if ((((uintptr_t)Q | (uintptr_t)Kpages | (uintptr_t)Vpages | (uintptr_t)O | (uintptr_t)workspace) & 15) != 0) return LOTTS_ERR_SHAPE;
-    if ((((uintptr_t)page_table | (uintptr_t)kv_len | (uintptr_t)q_start | (uintptr_t)lse) & 3) != 0) return LOTTS_ERR_SHAPE;
-    const PagedPlan pl = paged_plan(d);
-    if (workspace_bytes < (d.dtype == LOTTS_F32 ? 256 : pl.bytes)) return LOTTS_ERR_WORKSPACE;
-    const long long es = d.dtype == LOTTS_BF16 ? 2 : 4;
-    PagedParams p;
+// Fills in what the kernels of both entry points take; es, cache_es: bytes of an element of Q and O, and of the cache.
+static void paged_params(PagedParams* pp, const lotts_paged_desc& d, int shift, const PagedPlan& pl, long long es, long long cache_es, const void* Q, const void* Kpages,
+                         const void* Vpages, const int32_t* page_table, const int32_t* kv_len, const int32_t* q_start, void* O, float* lse, void* workspace) {
+    PagedParams& p = *pp;
     p.Q = Q; p.K = Kpages; p.V = Vpages; p.table = page_table; p.kv_len = kv_len; p.q_start = q_start; p.O = O; p.lse = lse;
     p.q_t = d.q_stride_t * es; p.q_h = d.q_stride_h * es; p.o_t = d.o_stride_t * es; p.o_h = d.o_stride_h * es;
-    p.page_p = d.page_stride_p * es; p.page_h = d.page_stride_h * es; p.page_t = d.page_stride_t * es;
+    p.page_p = d.page_stride_p * cache_es; p.page_h = d.page_stride_h * cache_es; p.page_t = d.page_stride_t * cache_es;
     p.table_stride = d.table_stride;
     p.B = d.B; p.T = d.T; p.R = d.T / d.B; p.Hq = d.Hq; p.Hkv = d.Hkv; p.G = d.Hq / d.Hkv;
     p.pages = d.pages; p.columns = d.columns; p.shift = shift;
@@ -1357,18 +1360,99 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     p.ws = workspace; p.ws_bytes = (unsigned)pl.bytes; p.off_ml = (unsigned)pl.off_ml; p.off_o = (unsigned)pl.off_o;
     p.cells = static_cast<unsigned long long*>(workspace);
     p.tag = (g_paged_tag.fetch_add(1, std::memory_order_relaxed) + 1) << kPgTagShift;
+}
+
+// fp32: a row's keys are a chain of loads: few rows take 16 wavefronts each, so that the chain is short; many fill the chip with 4.  (80 rows of up to
+// 700 keys: 11.7 us a call with 4, 7.4 with 16.)
+template <typename T, typename P>
+static void paged_rows(const lotts_paged_desc& d, const P& p, hipStream_t s) {
+    const dim3 grid((unsigned)((long long)d.T * d.Hq));
+    if ((long long)d.T * d.Hq <= 2 * kNumCU) {
+        if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 16, P, T>), grid, dim3(16 * kWave), s, p);
+        else LOTTS_LAUNCH((paged_f32_kernel<128, 16, P, T>), grid, dim3(16 * kWave), s, p);
+    } else {
+        if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 4, P, T>), grid, dim3(4 * kWave), s, p);
+        else LOTTS_LAUNCH((paged_f32_kernel<128, 4, P, T>), grid, dim3(4 * kWave), s, p);
+    }
+}
+
+// The descriptor of a call over an MXFP8 cache; its scales' strides with the dense ones in the place of 0.
+static int paged_mx_desc(const lotts_paged_mx_desc* in, bool uniform, lotts_paged_mx_desc* d, int* shift) {
+    if (!in) return LOTTS_ERR_NULL;
+    const int rc = paged_desc(&in->paged, uniform, true, &d->paged, shift);
+    if (rc != LOTTS_OK) return rc;
+    const long long row = d->paged.D / kMxBlock;
+    d->scale_stride_p = in->scale_stride_p ? in->scale_stride_p : d->paged.Hkv * d->paged.page_tokens * row;
+    d->scale_stride_h = in->scale_stride_h ? in->scale_stride_h : d->paged.page_tokens * row;
+    d->scale_stride_t = in->scale_stride_t ? in->scale_stride_t : row;
+    for (long long s : {d->scale_stride_p, d->scale_stride_h, d->scale_stride_t})
+        if (s < 0) return LOTTS_ERR_SHAPE;
+    if (d->scale_stride_t < row || d->scale_stride_t > (1LL << 26)) return LOTTS_ERR_SHAPE;
+    return LOTTS_OK;
+}
+
+}  // namespace lotts
+
+extern "C" size_t verify_attention_paged_workspace_bytes(const lotts_paged_desc* desc) {
+    using namespace lotts;
+    lotts_paged_desc d;
+    int shift;
+    if (paged_desc(desc, false, false, &d, &shift) != LOTTS_OK) return 0;
+    return d.dtype == LOTTS_F32 ? 256 : paged_plan(d).bytes;
+}
+
+extern "C" size_t verify_attention_paged_mxfp8_workspace_bytes(const lotts_paged_mx_desc* desc) {
+    using namespace lotts;
+    lotts_paged_mx_desc d;
+    int shift;
+    if (paged_mx_desc(desc, false, &d, &shift) != LOTTS_OK) return 0;
+    return 256;
+}
+
+extern "C" int verify_attention_paged_mxfp8(const lotts_paged_mx_desc* desc, const void* Q, const void* Kpages, const void* Vpages, const void* Kscales,
+                                            const void* Vscales, const int32_t* page_table, const int32_t* kv_len, const int32_t* q_start, void* O, float* lse,
+                                            void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace lotts;
+    lotts_paged_mx_desc mx;
+    int shift;
+    const int rc = paged_mx_desc(desc, !q_start, &mx, &shift);
+    if (rc != LOTTS_OK) return rc;
+    const lotts_paged_desc& d = mx.paged;
+    if (!Q || !Kpages || !Vpages || !Kscales || !Vscales || !page_table || !kv_len || !O || !workspace) return LOTTS_ERR_NULL;
+    if ((((uintptr_t)Q | (uintptr_t)Kpages | (uintptr_t)Vpages | (uintptr_t)O | (uintptr_t)workspace) & 15) != 0) return LOTTS_ERR_SHAPE;
+    if ((((uintptr_t)page_table | (uintptr_t)kv_len | (uintptr_t)q_start | (uintptr_t)lse) & 3) != 0) return LOTTS_ERR_SHAPE;
+    const PagedPlan pl = paged_plan(d);
+    if (workspace_bytes < 256) return LOTTS_ERR_WORKSPACE;
+    PagedMxParams p;
+    paged_params(&p, d, shift, pl, d.dtype == LOTTS_BF16 ? 2 : 4, 1, Q, Kpages, Vpages, page_table, kv_len, q_start, O, lse, workspace);
+    p.Ks = static_cast<const unsigned char*>(Kscales);
+    p.Vs = static_cast<const unsigned char*>(Vscales);
+    p.scale_p = mx.scale_stride_p; p.scale_h = mx.scale_stride_h; p.scale_t = mx.scale_stride_t;
+    const hipStream_t s = (hipStream_t)stream;
+    if (d.dtype == LOTTS_F32) paged_rows<float>(d, p, s);
+    else paged_rows<__bf16>(d, p, s);
+    return check_launch();
+}
+
+extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* Q, const void* Kpages, const void* Vpages, const int32_t* page_table,
+                                      const int32_t* kv_len, const int32_t* q_start, void* O, float* lse, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+    using namespace lotts;
+    lotts_paged_desc d;
+    int shift;
+    const int rc = paged_desc(desc, !q_start, false, &d, &shift);
+    if (rc != LOTTS_OK) return rc;
+    if (!Q || !Kpages || !Vpages || !page_table || !kv_len || !O || !workspace) return LOTTS_ERR_NULL;
+    if ((((uintptr_t)Q | (uintptr_t)Kpages | (uintptr_t)Vpages | (uintptr_t)O | (uintptr_t)workspace) & 15) != 0) return LOTTS_ERR_SHAPE;
+    if ((((uintptr_t)page_table | (uintptr_t)kv_len | (uintptr_t)q_start | (uintptr_t)lse) & 3) != 0) return LOTTS_ERR_SHAPE;
+    const PagedPlan pl = paged_plan(d);
+    if (workspace_bytes < (d.dtype == LOTTS_F32 ? 256 : pl.bytes)) return LOTTS_ERR_WORKSPACE;
+    const long long es = d.dtype == LOTTS_BF16 ? 2 : 4;
+    PagedParams p;
+    paged_params(&p, d, shift, pl, es, es, Q, Kpages, Vpages, page_table, kv_len, q_start, O, lse, workspace);
     const hipStream_t s = (hipStream_t)stream;
     if (d.dtype == LOTTS_F32) {
-        const dim3 grid((unsigned)((long long)d.T * d.Hq));
-        // A row's keys are a chain of loads: few rows take 16 wavefronts each, so that the chain is short; many fill the chip with 4.  (80 rows of up to
-        // 700 keys: 11.7 us a call with 4, 7.4 with 16.)
-        if ((long long)d.T * d.Hq <= 2 * kNumCU) {
-            if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 16>), grid, dim3(16 * kWave), s, p);
-            else LOTTS_LAUNCH((paged_f32_kernel<128, 16>), grid, dim3(16 * kWave), s, p);
-        } else {
-            if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 4>), grid, dim3(4 * kWave), s, p);
-            else LOTTS_LAUNCH((paged_f32_kernel<128, 4>), grid, dim3(4 * kWave), s, p);
-        }
+        paged_rows<float>(d, p, s);
         return check_launch();
     }
     const dim3 grid((unsigned)pl.workers), block(paged_waves<false>() * kWave);
