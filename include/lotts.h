@@ -483,7 +483,7 @@ size_t verify_attention_paged_mxfp8_workspace_bytes(const lotts_paged_mx_desc *d
 
 /*
  * verify_attention_paged_mxfp8 -- verify_attention_paged over a cache in MXFP8, as kv_append_paged_mxfp8 writes it: half of the bytes to read.
- *   Kpages, Vpages [pages][Hkv][page_tokens][D] bytes, 16-byte aligned; Kscales, Vscales [pages][Hkv][page_tokens][D / 32] bytes
+ *   Kpages, Vpages [pages][Hkv][page_tokens][D] bytes, 16-byte aligned; Kscales, Vscales [pages][Hkv][page_tokens][D / 32] bytes, D / 32 bytes aligned
  *   the other arguments, the workspace (zero-filled once, then this entry point's own) and what holds for all of them: as for verify_attention_paged
  * The cached values are exact in bf16 and are multiplied as such (bf16 Q) or as fp32 (fp32 Q).  A NaN in V reaches the rows that see its key and no others.
  */

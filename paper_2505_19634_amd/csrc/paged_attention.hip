@@ -70,6 +70,9 @@ struct PagedMxParams : PagedParams {
     long long scale_p, scale_h, scale_t;  // bytes
 };
 
+template <typename P>
+constexpr bool kMx = std::is_same<P, PagedMxParams>::value;
+
 // A branch of the call: its first row of Q, its new tokens and all its tokens (both brought into the range that the arguments allow, so
 // that nothing is addressed out of bounds whatever the device data say).
 struct Branch {
@@ -291,6 +294,13 @@ __device__ __forceinline__ unsigned group_bytes(const PagedParams& p, int entry,
 __device__ __forceinline__ long long group_at(const PagedParams& p, int entry, int key, int kvh) {
     return (long long)((unsigned)entry < (unsigned)p.pages ? entry : 0) * p.page_p + kvh * p.page_h + (key & ((1 << p.shift) - 1)) * p.page_t;
 }
+// The same for the scales of an MXFP8 cache: how many of up to `most` keys there are, and where the first one's scales lie.
+__device__ __forceinline__ int group_keys(const PagedParams& p, int entry, int key, int keys, int most) {
+    return (unsigned)entry < (unsigned)p.pages ? max(0, min(keys - key, most)) : 0;
+}
+__device__ __forceinline__ long long scales_at(const PagedMxParams& p, int entry, int key, int kvh) {
+    return (long long)((unsigned)entry < (unsigned)p.pages ? entry : 0) * p.scale_p + kvh * p.scale_h + (key & ((1 << p.shift) - 1)) * p.scale_t;
+}
 
 // ---------------------------------------------------------------------------------------------
 // bf16
@@ -401,6 +411,44 @@ __device__ __forceinline__ bf16x8 read_v(unsigned at, int kk, int db) {  // A op
     return f.v;
 }
 
+// A wide item's keys of an MXFP8 cache come through registers: a wavefront's 8 rows of a tile, D / 8 codes a lane with their scale, become bf16 on the way into LDS,
+// where they lie as a bf16 cache's do.
+template <int D>
+struct MxRows {
+    static constexpr int BYTES = D / 8;
+    u32x4 codes;
+    unsigned scale;
+    // keys: how many of the rows there are; the others read as zeros
+    __device__ __forceinline__ void fetch(const unsigned char* c, const unsigned char* s, int keys, unsigned page_t, unsigned scale_t, int lane) {
+        const unsigned row = lane / 8, col = lane % 8 * BYTES, at = row * page_t + col;
+        const __amdgpu_buffer_rsrc_t cr = buffer(c, keys > 0 ? (unsigned)(keys - 1) * page_t + D : 0), sr = buffer(s, keys > 0 ? (unsigned)(keys - 1) * scale_t + D / kMxBlock : 0);
+        if constexpr (BYTES == 16) {
+            codes = __builtin_amdgcn_raw_buffer_load_b128(cr, (int)at, 0, 0);
+        } else {
+            const u32x2 half = __builtin_amdgcn_raw_buffer_load_b64(cr, (int)at, 0, 0);
+            codes[0] = half[0];
+            codes[1] = half[1];
+        }
+        scale = __builtin_amdgcn_raw_buffer_load_b8(sr, (int)(row * scale_t + col / kMxBlock), 0, 0);
+    }
+    // to: where the first row lies in LDS; r0: which one it is of the 16 that spread() counts
+    __device__ __forceinline__ void put(unsigned to, int r0, int lane) const {
+        const int r = lane / 8, sp = spread<D>(r0 + r);
+#pragma unroll
+        for (int c = 0; c < BYTES / 8; ++c)
+            *(__attribute__((address_space(3))) bf16x8*)(uintptr_t)(to + r * (D * 2) + ((lane % 8 * (BYTES / 8) + c) ^ sp) * 16) =
+                __builtin_bit_cast(bf16x8, mx_of_e4m3(codes[2 * c], codes[2 * c + 1], scale));
+    }
+};
+// A narrow item's codes lie in LDS as they come, D bytes a row, pieces of 16 bytes exchanged as spread() does for rows of as many bytes.
+template <int D>
+__device__ __forceinline__ int spread_codes(int r) {
+    if (D == 128) return spread<64>(r);
+    return r >> 2 & 3;  // 4 pieces a row, four rows next to each other
+}
+// The s-th of a row's scales, which are one load.
+__device__ __forceinline__ unsigned scale_of(unsigned row, int s) { return row >> (8 * s) & 0xff; }
+
 // Infinities and NaN in V.  A row's weight for a later token of its chunk is 0, but the product with V takes it all the same, and 0 times an infinity is
 // NaN.  So where some rows of an item do not see a key, what is not finite in the key's row of V is taken out of LDS before the products, and the rows that
 // see it get NaN in its columns afterwards.  (Looking costs the drafts of 16 branches 0.2 %, a prompt of 2039 0.8 %, one of 1500 with as many KV heads as
@@ -428,15 +476,25 @@ struct NotFinite {
 #pragma unroll
         for (int i = 0; i < C; ++i) first[i] = 0x7fffffff;
     }
-    __device__ __forceinline__ void look(const PagedParams& p, const int32_t* row, int kvh, int from, int to) {  // the later, the larger the keys
+    template <typename P>
+    __device__ __forceinline__ void look(const P& p, const int32_t* row, int kvh, int from, int to) {  // the later, the larger the keys
 #pragma unroll 4
         for (int key = from; key < to; ++key) {
             const int e = page_entry(p, row, key);
             const bool there = (unsigned)e < (unsigned)p.pages;  // (in no page: that of page 0 is read for nothing)
-            const unsigned short* v = reinterpret_cast<const unsigned short*>((const unsigned char*)p.V + group_at(p, e, key, kvh)) + (threadIdx.x & (kWave - 1)) * C;
+            if constexpr (kMx<P>) {
+                const int column = (threadIdx.x & (kWave - 1)) * C;
+                const unsigned char* v = (const unsigned char*)p.V + group_at(p, e, key, kvh) + column;
+                const float scale = mx_power(p.Vs[scales_at(p, e, key, kvh) + column / kMxBlock]);
 #pragma unroll
-            for (int i = 0; i < C; ++i)
-                if (there && (v[i] & 0x7f80) == 0x7f80) first[i] = min(first[i], key);
+                for (int i = 0; i < C; ++i)
+                    if (there && (__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)v[i], scale, false)) & 0x7f80) == 0x7f80) first[i] = min(first[i], key);
+            } else {
+                const unsigned short* v = reinterpret_cast<const unsigned short*>((const unsigned char*)p.V + group_at(p, e, key, kvh)) + (threadIdx.x & (kWave - 1)) * C;
+#pragma unroll
+                for (int i = 0; i < C; ++i)
+                    if (there && (v[i] & 0x7f80) == 0x7f80) first[i] = min(first[i], key);
+            }
         }
     }
     // at: D words of LDS that are the wavefront's.
@@ -459,22 +517,29 @@ struct NotFinite {
 
 // A narrow item's part: wavefront w takes tiles lo + w, lo + w + WAVES, ..., through STAGES slabs of its own: with two, the next tile is on its way while
 // one is worked on; with one, the other wavefronts' are.
-template <int D, int TW, int WAVES, int STAGES>
-__device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segment& g, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh_bad, int (*sh_first)[D], int* sh) {
+// Of an MXFP8 cache the codes get into LDS that way, D / 32 scales a key into a register of the key's lane.  V becomes bf16 in LDS, where it lies as a bf16 cache's does; K does
+// on its way to the products: a lane has a key's row there and takes 16 codes at a time, so the two products behind them have 8 each, and Q's fragments are
+// chosen to match.  What a product multiplies with what in which of its places does not matter.  Everything of a tile has been read from LDS before its products,
+// and the next one is on its way under them.
+template <typename P, int D, int TW, int WAVES, int STAGES>
+__device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh_bad, int (*sh_first)[D], int* sh) {
     using X = Tile<D>;
+    constexpr bool MX = kMx<P>;
     constexpr int ROW = D * 2, HALF = kNarrowTile * ROW, SLAB = narrow_slab<D>(STAGES), LOADS = 4 * X::NLD;  // of a tile
+    constexpr int CODES = kNarrowTile * D, LPR = MX ? D / 16 : X::LPR, RPI = kWave / LPR, NLD = kPgGroup / RPI;  // an MXFP8 slab: K's codes, V's, V
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
     const int ln = lane & 31, hh = lane >> 5;
     const int32_t* row = p.table + g.b * p.table_stride;
     const int keys = min(g.L, max(0, g.L - g.n + quot(g.nrows - 1, p.d_g) + 1)), before = g.L - g.n;
     const int n_tiles = g.lo + wave < g.hi ? (g.hi - 1 - g.lo - wave) / WAVES + 1 : 0;
-    const int v_row = lane / X::LPR, v_slot = lane % X::LPR;
+    const int v_row = lane / LPR, v_slot = lane % LPR;
     const unsigned slab = lds_address(lds) + wave * SLAB, row_off = (unsigned)v_row * (unsigned)p.page_t;
-    const unsigned piece = (v_slot ^ spread<D>(v_row)) * 16;  // of the first load; the others' differ in the bits that spread() takes from the row's upper part
+    const unsigned piece = (v_slot ^ (MX ? spread_codes<D>(v_row) : spread<D>(v_row))) * 16;  // of the first load; the others' differ in the bits that spread() takes from the row's upper part
     // Lane i knows of the wavefront's tile ahead_from + i where its two groups of 16 keys lie and how many bytes of them there are (none
     // without a page, and behind the last key).
-    unsigned ahead_lo[2], ahead_hi[2], ahead_bytes[2];
+    unsigned ahead_lo[2], ahead_hi[2], ahead_bytes[2], ahead_scale_lo[2], ahead_scale_hi[2];
     int ahead_from = 0;
+    unsigned next_scales = 0;  // of key lane % 32 of the next tile: K's, or V's in the upper half
     auto look_ahead = [&](int it) {
         ahead_from = it;
 #pragma unroll
@@ -483,7 +548,12 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             const long long at = group_at(p, e, key, g.kvh);
             ahead_lo[h] = (unsigned)at;
             ahead_hi[h] = (unsigned)(at >> 32);
-            ahead_bytes[h] = group_bytes(p, e, key, keys, D * 2) | ((unsigned)e < (unsigned)p.pages ? 1u : 0u);  // (a multiple of 16; bit 0: it has a page)
+            if constexpr (MX) {
+                const long long scale = scales_at(p, e, key, g.kvh);
+                ahead_scale_lo[h] = (unsigned)scale;
+                ahead_scale_hi[h] = (unsigned)(scale >> 32);
+            }
+            ahead_bytes[h] = group_bytes(p, e, key, keys, MX ? D : D * 2) | ((unsigned)e < (unsigned)p.pages ? 1u : 0u);  // (a multiple of 16; bit 0: it has a page)
         }
     };
     auto fetch = [&](int it) {
@@ -491,6 +561,19 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
         const int x = it - ahead_from;
         const unsigned stage = slab + (STAGES > 1 ? (it & 1) * 2 * HALF : 0);
         int have = 0;
+        if constexpr (MX) {  // (the codes' waits count the scales)
+            const int group = ln / kPgGroup, r = ln & (kPgGroup - 1);
+            unsigned long long at[2];
+            int n[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                at[h] = (unsigned long long)(unsigned)__builtin_amdgcn_readlane(ahead_scale_hi[h], x) << 32 | (unsigned)__builtin_amdgcn_readlane(ahead_scale_lo[h], x);
+                n[h] = __builtin_amdgcn_readlane(ahead_bytes[h], x) & ~1 ? keys - (g.lo + wave + it * WAVES) * kNarrowTile - h * kPgGroup : 0;
+            }
+            const unsigned char* from = (hh ? p.Vs : p.Ks) + (long long)(group ? at[1] : at[0]) + (unsigned)r * (unsigned)p.scale_t;
+            next_scales = 0;
+            if (r < (group ? n[1] : n[0])) next_scales = D == 128 ? *reinterpret_cast<const unsigned*>(from) : *reinterpret_cast<const unsigned short*>(from);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long long at = (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane(ahead_hi[h], x) << 32 | (unsigned)__builtin_amdgcn_readlane(ahead_lo[h], x));
@@ -498,10 +581,10 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
             have |= (int)(bytes & 1) << h;
             const __amdgpu_buffer_rsrc_t kr = buffer((const unsigned char*)p.K + at, bytes & ~1u), vr = buffer((const unsigned char*)p.V + at, bytes & ~1u);
 #pragma unroll
-            for (int i = 0; i < X::NLD; ++i) {
-                const unsigned off = row_off + (unsigned)(i * X::RPI) * (unsigned)p.page_t + (piece ^ spread<D>(i * X::RPI) * 16);
-                load_to_lds<true>(kr, off, stage + h * kPgGroup * ROW + i * 1024);
-                load_to_lds<true>(vr, off, stage + HALF + h * kPgGroup * ROW + i * 1024);
+            for (int i = 0; i < NLD; ++i) {
+                const unsigned off = row_off + (unsigned)(i * RPI) * (unsigned)p.page_t + (piece ^ (MX ? spread_codes<D>(i * RPI) : spread<D>(i * RPI)) * 16);
+                load_to_lds<true>(kr, off, stage + h * kPgGroup * (MX ? D : ROW) + i * 1024);
+                load_to_lds<true>(vr, off, stage + (MX ? CODES : HALF) + h * kPgGroup * (MX ? D : ROW) + i * 1024);
             }
         }
         return have;
@@ -519,12 +602,14 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
         lim[t] = before + i + 1;
         const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
 #pragma unroll
-        for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + hh) * 16);
+        for (int s = 0; s < X::KS; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + (MX ? (s & ~1) * 2 + hh * 2 + (s & 1) : 2 * s + hh) * 16);
     }
     const bool two = TW > 1 && g.nrows > 32;
     bool taken_out = false;
     const int unseen = g.n > 1 ? (before + 1) & -X::RPI : 0x7fffffff;  // keys that not all rows see, and those that a load brings with them
     const unsigned kat = slab + lane_of_k<D>(lane), vat = slab + HALF + lane_of_v<D>(lane);
+    // an MXFP8 slab: the lane's key's codes of K, and V behind both operands' codes (HALF bytes): pieces differ in bits of the address that the row does not touch
+    const unsigned codes_at = slab + ln * D + (hh ^ spread_codes<D>(ln)) * 16, v_at = slab + HALF + ln * ROW + (hh * 2 ^ spread<D>(ln & 15)) * 16;
     f32x16 oacc[TW][X::DB];
     float m_run[TW], l_run[TW];
 #pragma unroll
@@ -539,7 +624,26 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
     for (int it = 0; it < n_tiles; ++it) {
         const int kb = (g.lo + wave + it * WAVES) * kNarrowTile, have = have_next;
         const unsigned stage = STAGES > 1 ? (it & 1) * 2 * HALF : 0;
-        if (STAGES > 1 && it + 1 < n_tiles) {
+        bf16x8 kf[X::KS], pf[TW][2];
+        if constexpr (MX) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            const u32x2 scales = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(next_scales, next_scales, false, false));  // K's, V's of key ln
+            u32x4 kc[X::KS / 2], vc[X::KS / 2];
+#pragma unroll
+            for (int s = 0; s < X::KS / 2; ++s) {
+                vc[s] = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(codes_at + CODES ^ s * 32);
+                kc[s] = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(codes_at ^ s * 32);
+            }
+#pragma unroll
+            for (int s = 0; s < X::KS / 2; ++s)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    *(__attribute__((address_space(3))) bf16x8*)(uintptr_t)(v_at ^ (s * 64 + c * 16)) = __builtin_bit_cast(bf16x8, mx_of_e4m3(vc[s][2 * c], vc[s][2 * c + 1], scale_of(scales[1], s)));
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (it + 1 < n_tiles) have_next = fetch(it + 1);
+#pragma unroll
+            for (int s = 0; s < X::KS; ++s) kf[s] = __builtin_bit_cast(bf16x8, mx_of_e4m3(kc[s / 2][2 * (s & 1)], kc[s / 2][2 * (s & 1) + 1], scale_of(scales[0], s / 2)));
+        } else if (STAGES > 1 && it + 1 < n_tiles) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile before has been read
             have_next = fetch(it + 1);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
@@ -552,9 +656,10 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
                 taken_out |= keep_finite(slab + stage + HALF + (key - kb) * ROW + lane * 16);
         }
         const bool masked = have != 3 || kb + kNarrowTile > before + 1;
-        bf16x8 kf[X::KS], pf[TW][2];
+        if constexpr (!MX) {
 #pragma unroll
-        for (int s = 0; s < X::KS; ++s) kf[s] = read_k<D>(kat + stage, s);
+            for (int s = 0; s < X::KS; ++s) kf[s] = read_k<D>(kat + stage, s);
+        }
 #pragma unroll
         for (int t = 0; t < TW; ++t) {
             if (t > 0 && !two) continue;
@@ -574,7 +679,7 @@ __device__ __forceinline__ void narrow_segment(const PagedParams& p, const Segme
                 for (int t = 0; t < TW; ++t)
                     if (t == 0 || two) oacc[t][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[t][kk], oacc[t][db], 0, 0, 0);
             }
-        if (STAGES == 1 && it + 1 < n_tiles) {
+        if (!MX && STAGES == 1 && it + 1 < n_tiles) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             have_next = fetch(it + 1);
         }
@@ -685,13 +790,14 @@ __device__ __forceinline__ void mfma_done(f32x16 (&d)[N]) {
 // that nothing in a slot depends on anything else in it; scheduling barriers keep the slots apart.  Loads go out a few a step: all of a tile's at
 // once held the wavefronts 1000 to 1600 cycles a tile.  (4 wavefronts of two row tiles, a SIMD each: a prompt of 2039 tokens,
 // 16 / 2 heads, 81 us against 62 with 8; 2 chunks of 2048 alike.)
-template <int D, typename Arrive, typename Request>
+// LOADS: what a wavefront requests of a tile's K and V in the slots (of an MXFP8 cache nothing: arrive() does).
+template <int D, int LOADS, typename Arrive, typename Request>
 __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[Tile<D>::KS], int lim,
                                           int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[Tile<D>::DB], float& m, float& l, Arrive arrive, Request request) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
     constexpr int QS = X::KS, VS = 2 * X::DB;   // slots: products of 32 keys with K and with V
-    constexpr int LOADS = wide_loads<D>(), EARLY = LOADS / 2;  // of a wavefront and operand; those beside products with K
+    constexpr int EARLY = LOADS / 2;            // those beside products with K
     constexpr int AHEAD = 3;                    // slots between a read from LDS and its use
     constexpr int PAIRS = 8;                    // pairs of weights: the first half goes into the first half of the products with V
     constexpr int SPAN = QS + X::DB - (D == 64 ? 3 : 2);  // slots over which they begin: done two slots before their product
@@ -822,7 +928,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int r = EARLY; r < LOADS; ++r)
-                if (i == (2 * (r - EARLY) + 1) * VS / (2 * (LOADS - EARLY))) request((j >> 1) + 2, j & 1, r);
+                if (i == (2 * (r - EARLY) + 1) * VS / (2 * (LOADS > EARLY ? LOADS - EARLY : 1))) request((j >> 1) + 2, j & 1, r);
         }
         settle();
     };
@@ -868,8 +974,8 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
 }
 
 // The workgroup loads a tile together, 8 keys a wavefront; wavefront w takes row tile w of the item.
-template <int D, int WAVES>
-__device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment& g, unsigned char* lds, int* sh, int* sh_bad) {
+template <typename P, int D, int WAVES>
+__device__ __forceinline__ void wide_segment(const P& p, const Segment& g, unsigned char* lds, int* sh, int* sh_bad) {
     using X = Tile<D>;
     constexpr int KEYS = kWideTile / WAVES, LOADS = wide_loads<D>();
     static_assert(WAVES * 32 == kWideRows && KEYS * WAVES == kWideTile && KEYS <= kPgGroup && KEYS == LOADS * X::RPI, "a row tile and some keys of a tile for every wavefront");
@@ -883,8 +989,9 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     const int v_row = lane / X::LPR, v_slot = lane % X::LPR;
     // Lane i knows of tile ahead_from + i: where the wavefront's keys lie, how many bytes of them there are (none without a page, and behind
     // the last key), and which of the tile's four groups have a page.
-    unsigned ahead_lo = 0, ahead_hi = 0, ahead_bytes = 0;
+    unsigned ahead_lo = 0, ahead_hi = 0, ahead_bytes = 0, ahead_scale_lo = 0, ahead_scale_hi = 0;
     int ahead_have = 0, ahead_from = 0;
+    MxRows<D> k8, v8;  // an MXFP8 cache's next tile
     auto look_ahead = [&](int it) {
         ahead_from = it;
         ahead_have = 0;
@@ -899,6 +1006,12 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
                 ahead_lo = (unsigned)at;
                 ahead_hi = (unsigned)(at >> 32);
                 ahead_bytes = group_bytes(p, e, key, min(keys, key + KEYS), D * 2);
+                if constexpr (kMx<P>) {
+                    const long long scale = scales_at(p, e, key, g.kvh);
+                    ahead_scale_lo = (unsigned)scale;
+                    ahead_scale_hi = (unsigned)(scale >> 32);
+                    ahead_bytes = group_keys(p, e, key, keys, KEYS);
+                }
             }
         }
     };
@@ -909,6 +1022,18 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     const unsigned long long k_to_v = (unsigned long long)p.V - (unsigned long long)p.K;
     unsigned long long at = 0;
     unsigned bytes = 0, stage = 0;
+    auto fetch8 = [&](int it) {
+        if constexpr (kMx<P>) {
+            if (it - ahead_from >= kWave) look_ahead(it);
+            const int x = it - ahead_from;
+            at = (unsigned long long)(unsigned)__builtin_amdgcn_readlane(ahead_hi, x) << 32 | (unsigned)__builtin_amdgcn_readlane(ahead_lo, x);
+            const unsigned long long scale = (unsigned long long)(unsigned)__builtin_amdgcn_readlane(ahead_scale_hi, x) << 32 | (unsigned)__builtin_amdgcn_readlane(ahead_scale_lo, x);
+            const int n = __builtin_amdgcn_readlane(ahead_bytes, x);
+            have_0 = __builtin_amdgcn_readlane(ahead_have, x);
+            k8.fetch((const unsigned char*)p.K + (long long)at, p.Ks + (long long)scale, n, (unsigned)p.page_t, (unsigned)p.scale_t, lane);
+            v8.fetch((const unsigned char*)p.V + (long long)at, p.Vs + (long long)scale, n, (unsigned)p.page_t, (unsigned)p.scale_t, lane);
+        }
+    };
     // Tiles behind the last one are requested too, with no bytes in range: every wait counts the same loads.
     auto request = [&](int it, int v, int i) {
         if (i == 0 && v == 0) {
@@ -928,17 +1053,39 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
     int until_unseen = max(0, (unseen - wave * KEYS + kWideTile - 1) / kWideTile) - g.lo;  // tiles to arrive in front of the first one in which the wavefront has such keys
     sh_bad[wave] = 0;  // (whether the wavefront has taken something out of V)
     look_ahead(g.lo);
+    if constexpr (kMx<P>) {
+        fetch8(g.lo);
+    } else {
 #pragma unroll
-    for (int tile = 0; tile < 2; ++tile) {
+        for (int tile = 0; tile < 2; ++tile) {
 #pragma unroll
-        for (int v = 0; v < 2; ++v)
+            for (int v = 0; v < 2; ++v)
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) request(g.lo + tile, v, i);
-        if (tile == 0) have_0 = have_1;
+                for (int i = 0; i < LOADS; ++i) request(g.lo + tile, v, i);
+            if (tile == 0) have_0 = have_1;
+        }
     }
+    int arrives = g.lo;  // the tile that arrives next
     // The next tile is in LDS for everybody; everybody has left the tile before the last behind, whose stage the next requests take.  Loads behind
     // the tile's that are on their way: K and V of the next one at first, then K and half of V of the next one.
+    // An MXFP8 cache's next tile goes from registers to LDS here, and the one behind it is requested: nobody reads its stage any more, the slowest wavefront is at the
+    // tile before the last.
     auto arrive_tile = [&](bool first, unsigned stage_at) {
+        if constexpr (kMx<P>) {
+            const int have = have_0;
+            k8.put(to + stage_at, wave * KEYS, lane);
+            v8.put(to + stage_at + HALF, wave * KEYS, lane);
+            if (++arrives < g.hi) fetch8(arrives);
+            if (__builtin_expect(--until_unseen < 0, 0)) {
+                asm volatile("" ::: "memory");
+                bool taken_out = false;
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) taken_out |= keep_finite(to + stage_at + HALF + i * 1024 + lane * 16);
+                if (taken_out) sh_bad[wave] = 1;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            return have;
+        }
         if (__builtin_expect(--until_unseen < 0, 0)) {
             if (first) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
             else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS + LOADS / 2) : "memory");
@@ -966,19 +1113,20 @@ __device__ __forceinline__ void wide_segment(const PagedParams& p, const Segment
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     if (wave * 32 < g.nrows) {
-        wide_rows<D>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
+        wide_rows<D, kMx<P> ? 0 : LOADS>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
     } else {  // no rows: the loads and the meetings alone, in the same order
+        constexpr int N = kMx<P> ? 0 : LOADS;
         arrive_tile(true, g.lo % kStages * STAGE);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) request(g.lo + 2, 0, i);
+        for (int i = 0; i < N; ++i) request(g.lo + 2, 0, i);
         for (int j = g.lo; j + 1 < g.hi; ++j) {
 #pragma unroll
-            for (int i = 0; i < LOADS / 2; ++i) request(j + 2, 1, i);
+            for (int i = 0; i < N / 2; ++i) request(j + 2, 1, i);
             arrive_tile(false, (j + 1) % kStages * STAGE);
 #pragma unroll
-            for (int i = LOADS / 2; i < LOADS; ++i) request(j + 2, 1, i);
+            for (int i = N / 2; i < N; ++i) request(j + 2, 1, i);
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) request(j + 3, 0, i);
+            for (int i = 0; i < N; ++i) request(j + 3, 0, i);
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -1024,10 +1172,10 @@ template <bool WIDE>
 __host__ __device__ constexpr int paged_waves() {
     return WIDE ? 8 : 4;
 }
-template <int D, int NARROW_TILES, bool WIDE, bool TWO>
-__global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) void paged_attn_kernel(const PagedParams p) {
+template <typename P, int D, int NARROW_TILES, bool WIDE, bool TWO>
+__global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) void paged_attn_kernel(const P p) {
     constexpr int WAVES = paged_waves<WIDE>();
-    constexpr int STAGES = WIDE || (TWO && D == 128) ? 1 : 2, NARROW_LDS = WAVES * narrow_slab<D>(STAGES), WIDE_LDS = kStages * kWideTile * 2 * D * 2;
+    constexpr int STAGES = kMx<P> || WIDE || (TWO && D == 128) ? 1 : 2, NARROW_LDS = WAVES * narrow_slab<D>(STAGES), WIDE_LDS = kStages * kWideTile * 2 * D * 2;
     __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > NARROW_LDS ? WIDE_LDS : NARROW_LDS];
     __shared__ float sh_m[WAVES][32], sh_l[WAVES][32];
     __shared__ int sh, sh_bad[WAVES];  // sh_bad: whether a wavefront has taken something out of V; sh_first: NotFinite's, of a narrow item
@@ -1142,10 +1290,10 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) v
         g.hi = __builtin_amdgcn_readfirstlane(g.hi);
         if (g.lo >= g.hi) continue;
         if constexpr (WIDE) {
-            if (narrow) narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
-            else wide_segment<D, WAVES>(p, g, lds, &sh, sh_bad);
+            if (narrow) narrow_segment<P, D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
+            else wide_segment<P, D, WAVES>(p, g, lds, &sh, sh_bad);
         } else {
-            narrow_segment<D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
+            narrow_segment<P, D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
         }
     }
 }
@@ -1156,9 +1304,8 @@ __global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) v
 // the states meet at the end.  The maximum is that of the scores as they are and the differences from it are scaled, so that the largest weight is 1
 // whatever the scale.
 // ---------------------------------------------------------------------------------------------
-template <int D, int WAVES, typename P, typename T>
+template <int D, int WAVES, typename P>
 __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const P p) {
-    constexpr bool MX = std::is_same<P, PagedMxParams>::value;
     constexpr int LPK = D / 4, KPL = kWave / LPK, NJ = 4, CHUNK = NJ * KPL;
     __shared__ __attribute__((aligned(16))) float sh_acc[WAVES][D];
     __shared__ float sh_ml[WAVES][2];
@@ -1183,33 +1330,24 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const P p) {
     const int n = keys_of_row(branch_at(p, b), t);
     if (n < 0) return;
     const float scale = p.scale;
-    float4 qv;
-    {
-        const unsigned char* qp = (const unsigned char*)p.Q + t * p.q_t + h * p.q_h + c4 * (int)(4 * sizeof(T));
-        if constexpr (sizeof(T) == 2) {
-            const bf16x4 q4 = *reinterpret_cast<const bf16x4*>(qp);
-            qv = make_float4(q4[0], q4[1], q4[2], q4[3]);
-        } else {
-            qv = *reinterpret_cast<const float4*>(qp);
-        }
-    }
+    const float4 qv = *reinterpret_cast<const float4*>((const unsigned char*)p.Q + t * p.q_t + h * p.q_h + c4 * 16);
     const int32_t* row = p.table + b * p.table_stride;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float m = -INFINITY, l = 0.f;
     for (int j0 = wave * CHUNK; j0 < n; j0 += WAVES * CHUNK) {
         const int e = __builtin_amdgcn_readfirstlane(row[j0 >> p.shift]);
         if ((unsigned)e >= (unsigned)p.pages) continue;  // no page: nothing to see
-        const unsigned char* kp = (const unsigned char*)p.K + e * p.page_p + kvh * p.page_h + c4 * (MX ? 4 : 16);
-        const unsigned char* vp = (const unsigned char*)p.V + e * p.page_p + kvh * p.page_h + c4 * (MX ? 4 : 16);
+        const unsigned char* kp = (const unsigned char*)p.K + e * p.page_p + kvh * p.page_h + c4 * (kMx<P> ? 4 : 16);
+        const unsigned char* vp = (const unsigned char*)p.V + e * p.page_p + kvh * p.page_h + c4 * (kMx<P> ? 4 : 16);
         float4 kv[NJ], vv[NJ];
 #pragma unroll
         for (int i = 0; i < NJ; ++i) {
             const int j = min(j0 + i * KPL + grp, n - 1);  // keys behind the last one re-read it; masked below
             const long long off = (j & ((1 << p.shift) - 1)) * p.page_t;
-            if constexpr (MX) {
-                const long long scale_at = e * p.scale_p + kvh * p.scale_h + (j & ((1 << p.shift) - 1)) * p.scale_t + c4 / (kMxBlock / 4);
-                kv[i] = mx_f32_of_e4m3(*reinterpret_cast<const unsigned*>(kp + off), p.Ks[scale_at]);
-                vv[i] = mx_f32_of_e4m3(*reinterpret_cast<const unsigned*>(vp + off), p.Vs[scale_at]);
+            if constexpr (kMx<P>) {
+                const long long at = scales_at(p, e, j, kvh) + c4 / (kMxBlock / 4);
+                kv[i] = mx_f32_of_e4m3(*reinterpret_cast<const unsigned*>(kp + off), p.Ks[at]);
+                vv[i] = mx_f32_of_e4m3(*reinterpret_cast<const unsigned*>(vp + off), p.Vs[at]);
             } else {
                 kv[i] = *reinterpret_cast<const float4*>(kp + off);
                 vv[i] = *reinterpret_cast<const float4*>(vp + off);
@@ -1264,7 +1402,7 @@ __global__ __launch_bounds__(WAVES * kWave) void paged_f32_kernel(const P p) {
             lsum += sh_ml[w][1] * wgt;
             o += sh_acc[w][tid] * wgt;
         }
-        reinterpret_cast<T*>((unsigned char*)p.O + t * p.o_t + h * p.o_h)[tid] = (T)(lsum == 0.f ? 0.f : o / lsum);
+        reinterpret_cast<float*>((unsigned char*)p.O + t * p.o_t + h * p.o_h)[tid] = lsum == 0.f ? 0.f : o / lsum;
         if (p.lse && tid == 0) p.lse[(long long)t * p.Hq + h] = M * scale + logf(lsum);
     }
 }
@@ -1364,15 +1502,34 @@ static void paged_params(PagedParams* pp, const lotts_paged_desc& d, int shift, 
 
 // fp32: a row's keys are a chain of loads: few rows take 16 wavefronts each, so that the chain is short; many fill the chip with 4.  (80 rows of up to
 // 700 keys: 11.7 us a call with 4, 7.4 with 16.)
-template <typename T, typename P>
+template <typename P>
 static void paged_rows(const lotts_paged_desc& d, const P& p, hipStream_t s) {
     const dim3 grid((unsigned)((long long)d.T * d.Hq));
     if ((long long)d.T * d.Hq <= 2 * kNumCU) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 16, P, T>), grid, dim3(16 * kWave), s, p);
-        else LOTTS_LAUNCH((paged_f32_kernel<128, 16, P, T>), grid, dim3(16 * kWave), s, p);
+        if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 16, P>), grid, dim3(16 * kWave), s, p);
+        else LOTTS_LAUNCH((paged_f32_kernel<128, 16, P>), grid, dim3(16 * kWave), s, p);
     } else {
-        if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 4, P, T>), grid, dim3(4 * kWave), s, p);
-        else LOTTS_LAUNCH((paged_f32_kernel<128, 4, P, T>), grid, dim3(4 * kWave), s, p);
+        if (d.D == 64) LOTTS_LAUNCH((paged_f32_kernel<64, 4, P>), grid, dim3(4 * kWave), s, p);
+        else LOTTS_LAUNCH((paged_f32_kernel<128, 4, P>), grid, dim3(4 * kWave), s, p);
+    }
+}
+
+// bf16 rows: the kernel that the plan says.
+template <typename P>
+static void paged_tiles(const lotts_paged_desc& d, const PagedPlan& pl, const P& p, hipStream_t s) {
+    const dim3 grid((unsigned)pl.workers), block(paged_waves<false>() * kWave);
+    if (pl.wide) {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
+    } else if (pl.narrow_tiles == 2) {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 2, false, false>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 2, false, false>), grid, block, s, p);
+    } else if (pl.two) {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 1, false, true>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 1, false, true>), grid, block, s, p);
+    } else {
+        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 1, false, false>), grid, block, s, p);
+        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 1, false, false>), grid, block, s, p);
     }
 }
 
@@ -1386,7 +1543,7 @@ static int paged_mx_desc(const lotts_paged_mx_desc* in, bool uniform, lotts_page
     d->scale_stride_h = in->scale_stride_h ? in->scale_stride_h : d->paged.page_tokens * row;
     d->scale_stride_t = in->scale_stride_t ? in->scale_stride_t : row;
     for (long long s : {d->scale_stride_p, d->scale_stride_h, d->scale_stride_t})
-        if (s < 0) return LOTTS_ERR_SHAPE;
+        if (s < 0 || s % row != 0) return LOTTS_ERR_SHAPE;
     if (d->scale_stride_t < row || d->scale_stride_t > (1LL << 26)) return LOTTS_ERR_SHAPE;
     return LOTTS_OK;
 }
@@ -1406,7 +1563,7 @@ extern "C" size_t verify_attention_paged_mxfp8_workspace_bytes(const lotts_paged
     lotts_paged_mx_desc d;
     int shift;
     if (paged_mx_desc(desc, false, &d, &shift) != LOTTS_OK) return 0;
-    return 256;
+    return d.paged.dtype == LOTTS_F32 ? 256 : paged_plan(d.paged).bytes;
 }
 
 extern "C" int verify_attention_paged_mxfp8(const lotts_paged_mx_desc* desc, const void* Q, const void* Kpages, const void* Vpages, const void* Kscales,
@@ -1421,16 +1578,17 @@ extern "C" int verify_attention_paged_mxfp8(const lotts_paged_mx_desc* desc, con
     if (!Q || !Kpages || !Vpages || !Kscales || !Vscales || !page_table || !kv_len || !O || !workspace) return LOTTS_ERR_NULL;
     if ((((uintptr_t)Q | (uintptr_t)Kpages | (uintptr_t)Vpages | (uintptr_t)O | (uintptr_t)workspace) & 15) != 0) return LOTTS_ERR_SHAPE;
     if ((((uintptr_t)page_table | (uintptr_t)kv_len | (uintptr_t)q_start | (uintptr_t)lse) & 3) != 0) return LOTTS_ERR_SHAPE;
+    if (((uintptr_t)Kscales | (uintptr_t)Vscales) % (d.D / kMxBlock) != 0) return LOTTS_ERR_SHAPE;  // a row's scales are one load
     const PagedPlan pl = paged_plan(d);
-    if (workspace_bytes < 256) return LOTTS_ERR_WORKSPACE;
+    if (workspace_bytes < (d.dtype == LOTTS_F32 ? 256 : pl.bytes)) return LOTTS_ERR_WORKSPACE;
     PagedMxParams p;
     paged_params(&p, d, shift, pl, d.dtype == LOTTS_BF16 ? 2 : 4, 1, Q, Kpages, Vpages, page_table, kv_len, q_start, O, lse, workspace);
     p.Ks = static_cast<const unsigned char*>(Kscales);
     p.Vs = static_cast<const unsigned char*>(Vscales);
     p.scale_p = mx.scale_stride_p; p.scale_h = mx.scale_stride_h; p.scale_t = mx.scale_stride_t;
     const hipStream_t s = (hipStream_t)stream;
-    if (d.dtype == LOTTS_F32) paged_rows<float>(d, p, s);
-    else paged_rows<__bf16>(d, p, s);
+    if (d.dtype == LOTTS_F32) paged_rows(d, p, s);
+    else paged_tiles(d, pl, p, s);
     return check_launch();
 }
 
@@ -1452,22 +1610,9 @@ extern "C" int verify_attention_paged(const lotts_paged_desc* desc, const void* 
     paged_params(&p, d, shift, pl, es, es, Q, Kpages, Vpages, page_table, kv_len, q_start, O, lse, workspace);
     const hipStream_t s = (hipStream_t)stream;
     if (d.dtype == LOTTS_F32) {
-        paged_rows<float>(d, p, s);
+        paged_rows(d, p, s);
         return check_launch();
     }
-    const dim3 grid((unsigned)pl.workers), block(paged_waves<false>() * kWave);
-    if (pl.wide) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
-    } else if (pl.narrow_tiles == 2) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 2, false, false>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 2, false, false>), grid, block, s, p);
-    } else if (pl.two) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, false, true>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, false, true>), grid, block, s, p);
-    } else {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<64, 1, false, false>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<128, 1, false, false>), grid, block, s, p);
-    }
+    paged_tiles(d, pl, p, s);
     return check_launch();
 }

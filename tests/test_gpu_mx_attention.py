@@ -122,13 +122,13 @@ def test_as_many_tokens_of_every_branch(lotts, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [64, 128])
-def test_scales_that_begin_anywhere(lotts, D, dtype):
-    """Scale rows of odd pitch at odd addresses, code rows further apart than they are long."""
+def test_rows_that_lie_apart(lotts, D, dtype):
+    """Scale rows of three times their length, code rows further apart than they are long."""
     c = MxCache([4, 100, 1], [300, 160, 77], 8, 2, D, 16, dtype, seed=D)
     pages, Hkv, page = c.Kc.shape[:3]
     one = lotts.verify_attention_paged_mxfp8(c.Q, *c.cache, c.table, c.kv_len, c.q_start)
     wide = [torch.full((pages, Hkv, page + 1, D + 48), 0x7f, dtype=torch.uint8, device=DEV)[:, :, :page, 16:16 + D] for _ in range(2)]
-    odd = [torch.full((pages, Hkv, page, D // 32 + 3), 255, dtype=torch.uint8, device=DEV)[..., 1:1 + D // 32] for _ in range(2)]
+    odd = [torch.full((pages, Hkv, page, 3 * (D // 32)), 255, dtype=torch.uint8, device=DEV)[..., D // 32:2 * (D // 32)] for _ in range(2)]
     for t, s in zip(wide + odd, c.cache):
         t.copy_(s.view(torch.uint8))
     out = lotts.verify_attention_paged_mxfp8(c.Q, *wide, *odd, c.table, c.kv_len, c.q_start)

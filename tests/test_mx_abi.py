@@ -74,7 +74,7 @@ BAD = [dict(B=0), dict(B=4097, T=4097 * 4), dict(T=0), dict(max_new=0), dict(max
        dict(page_tokens=8), dict(page_tokens=48), dict(page_tokens=2048), dict(pages=0), dict(pages=(1 << 24) + 1), dict(columns=0), dict(columns=1 << 24),
        dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(q_stride_h=124), dict(q_stride_t=4), dict(o_stride_h=64),
        dict(page_stride_t=100), dict(page_stride_t=64), dict(page_stride_t=136), dict(page_stride_p=-16), dict(table_stride=69), dict(T=1 << 20, max_new=1 << 20),
-       dict(page_stride_t=1 << 27), dict(scales=(0, 0, 3)), dict(scales=(-1, 0, 0)), dict(scales=(0, -4, 0)), dict(scales=(0, 0, 1 << 27))]
+       dict(page_stride_t=1 << 27), dict(scales=(0, 0, 3)), dict(scales=(-1, 0, 0)), dict(scales=(0, -4, 0)), dict(scales=(0, 0, 1 << 27)), dict(scales=(0, 0, 6)), dict(scales=(0, 33, 0)), dict(scales=(66, 0, 0)), dict(scales=(0, 0, 5), D=64)]
 
 
 @pytest.mark.parametrize("kw", BAD)
@@ -101,10 +101,13 @@ def test_attention_is_refused(lib):
         a = list(ok)
         a[i] = at(8)
         assert call(d, *a) == -2, i
-    for i in (5, 6, 7, 9):
+    for i in (3, 4, 5, 6, 7, 9):
         a = list(ok)
         a[i] = at(2)
         assert call(d, *a) == -2, i
+    a = list(ok)
+    a[3] = at(1)
+    assert call(desc(D=64), *a) == -2
     a = list(ok)
     a[11] = need - 1
     assert call(d, *a) == -4
