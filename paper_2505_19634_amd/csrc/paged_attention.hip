@@ -1168,13 +1168,14 @@ __device__ __forceinline__ void wide_segment(const P& p, const Segment& g, unsig
     __syncthreads();
 }
 
-template <bool WIDE>
+// Wavefronts of a workgroup.  (Of an MXFP8 cache a tile is half as many bytes: eight have as much on the way as four with two slabs each.)
+template <typename P, int NARROW_TILES, bool WIDE, bool TWO>
 __host__ __device__ constexpr int paged_waves() {
-    return WIDE ? 8 : 4;
+    return WIDE || (kMx<P> && NARROW_TILES == 1 && !TWO) ? 8 : 4;
 }
 template <typename P, int D, int NARROW_TILES, bool WIDE, bool TWO>
-__global__ __launch_bounds__(paged_waves<WIDE>() * kWave, TWO || WIDE ? 2 : 1) void paged_attn_kernel(const P p) {
-    constexpr int WAVES = paged_waves<WIDE>();
+__global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave), TWO || WIDE ? 2 : 1) void paged_attn_kernel(const P p) {
+    constexpr int WAVES = paged_waves<P, NARROW_TILES, WIDE, TWO>();
     constexpr int STAGES = kMx<P> || WIDE || (TWO && D == 128) ? 1 : 2, NARROW_LDS = WAVES * narrow_slab<D>(STAGES), WIDE_LDS = kStages * kWideTile * 2 * D * 2;
     __shared__ __attribute__((aligned(256))) unsigned char lds[WIDE && WIDE_LDS > NARROW_LDS ? WIDE_LDS : NARROW_LDS];
     __shared__ float sh_m[WAVES][32], sh_l[WAVES][32];
@@ -1514,23 +1515,29 @@ static void paged_rows(const lotts_paged_desc& d, const P& p, hipStream_t s) {
     }
 }
 
+template <typename P, int D, int NARROW_TILES, bool WIDE, bool TWO>
+constexpr int paged_block() {
+    return paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave;
+}
 // bf16 rows: the kernel that the plan says.
 template <typename P>
 static void paged_tiles(const lotts_paged_desc& d, const PagedPlan& pl, const P& p, hipStream_t s) {
-    const dim3 grid((unsigned)pl.workers), block(paged_waves<false>() * kWave);
+    const dim3 grid((unsigned)pl.workers);
+#define PAGED_LAUNCH(...) LOTTS_LAUNCH((paged_attn_kernel<P, __VA_ARGS__>), grid, dim3(paged_block<P, __VA_ARGS__>()), s, p)
     if (pl.wide) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 1, true, false>), grid, dim3(paged_waves<true>() * kWave), s, p);
+        if (d.D == 64) PAGED_LAUNCH(64, 1, true, false);
+        else PAGED_LAUNCH(128, 1, true, false);
     } else if (pl.narrow_tiles == 2) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 2, false, false>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 2, false, false>), grid, block, s, p);
+        if (d.D == 64) PAGED_LAUNCH(64, 2, false, false);
+        else PAGED_LAUNCH(128, 2, false, false);
     } else if (pl.two) {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 1, false, true>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 1, false, true>), grid, block, s, p);
+        if (d.D == 64) PAGED_LAUNCH(64, 1, false, true);
+        else PAGED_LAUNCH(128, 1, false, true);
     } else {
-        if (d.D == 64) LOTTS_LAUNCH((paged_attn_kernel<P, 64, 1, false, false>), grid, block, s, p);
-        else LOTTS_LAUNCH((paged_attn_kernel<P, 128, 1, false, false>), grid, block, s, p);
+        if (d.D == 64) PAGED_LAUNCH(64, 1, false, false);
+        else PAGED_LAUNCH(128, 1, false, false);
     }
+#undef PAGED_LAUNCH
 }
 
 // The descriptor of a call over an MXFP8 cache; its scales' strides with the dense ones in the place of 0.
