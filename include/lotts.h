@@ -452,7 +452,8 @@ size_t skinny_gemm_mxfp4_workspace_bytes(int32_t M, int32_t N, int32_t K);
 /*
  * skinny_gemm_mxfp4 -- skinny_gemm against a weight matrix in MXFP4: Y[m][n] = sum_k X[m][k] * W[n][k], W what codes and scales stand for.
  *   X [M][K] bf16 (row pitch ldx elements), codes [N][K / 2] (ld_codes bytes), scales [N][K / 32] (ld_scales bytes), Y [M][N] bf16 out (ldy elements)
- *   1 <= M <= 256; any N; K a multiple of 32 (both up to 2^26); X, codes, workspace 16-byte aligned, ldx a multiple of 8, ld_codes of 16; Y and scales as they are
+ *   1 <= M <= 256; any N; K a multiple of 32 (both up to 2^22); X, codes, workspace 16-byte aligned, ldx a multiple of 8 up to 2^22, ld_codes of 16; Y and scales
+ *   as they are; ld_codes, ld_scales up to 2^24
  * The weights become bf16, exactly, and the products accumulate in fp32 on the matrix cores, in an order that the sizes decide: the same data give the same bits.
  *   workspace: >= skinny_gemm_mxfp4_workspace_bytes(M, N, K), any contents
  */
@@ -511,7 +512,7 @@ int verify_attention_paged_mxfp8(const lotts_paged_mx_desc *desc, const void *Q,
  * pick); majority_vote 1; confidence_vote 1; skinny_gemm 1 (2 when K is split: GEMM, reduce),
  * skinny_gemm_append the same (and kv_append where a product that streams W has K unsplit); verify_attention_paged 1; kv_append_paged 1;
  * kv_pages_reserve, _fork, _free, _copy 1; kv_pages_compact 2; mxfp4_quantize, mxfp4_dequantize, kv_append_paged_mxfp8,
- * verify_attention_paged_mxfp8 1; skinny_gemm_mxfp4 1.
+ * verify_attention_paged_mxfp8 1; skinny_gemm_mxfp4 1 (2 where K is split: product, reduce).
  */
 int lotts_timer_start(int32_t max_launches);
 int lotts_timer_pause(int32_t paused);

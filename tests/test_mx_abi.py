@@ -44,7 +44,8 @@ def test_product_is_refused(lib):
     for bad in (dict(x=None), dict(c=None), dict(s=None), dict(y=None), dict(w=None)):
         assert g(**bad) == -1, bad
     for bad in (dict(M=0), dict(M=257), dict(N=0), dict(K=48), dict(K=-64), dict(lx=63), dict(lx=68), dict(lc=31), dict(lc=40), dict(ls=1), dict(ly=39), dict(x=at(8)), dict(c=at(8)), dict(w=at(8)),
-                dict(y=at(1)), dict(N=1 << 27, ly=1 << 27), dict(lx=1 << 60), dict(lc=1 << 60), dict(ls=1 << 60), dict(ly=1 << 60)):
+                dict(y=at(1)), dict(N=(1 << 22) + 1, ly=1 << 27), dict(K=(1 << 22) + 32, lx=1 << 23, lc=1 << 22, ls=1 << 18),
+                dict(lx=(1 << 22) + 8), dict(lc=(1 << 24) + 16), dict(ls=(1 << 24) + 1), dict(ly=1 << 60)):
         assert g(**bad) == -2, bad
     assert g(wb=need(4, 40, 64) - 1) == -4
 
