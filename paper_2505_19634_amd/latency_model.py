@@ -17,6 +17,7 @@ one-token step of the target each (an assumption: a draft model a tenth of the t
 
     python -m paper_2505_19634_amd.latency_model --shape 3B --budget-s 4
     python -m paper_2505_19634_amd.latency_model --shape 32B --budget-s 20 --full-model 16,3
+    python -m paper_2505_19634_amd.latency_model --shape 32B --budget-s 0 --full-model 16,3 --microscaled
 """
 from __future__ import annotations
 
@@ -145,6 +146,22 @@ class FullModel:
         self.layers = [first] + [{k: v.clone() for k, v in first.items()} for _ in range(s.layers - 1)]
         self.lm_head = w(s.V, s.hidden)
         self.priv_len = torch.full((B,), private + R, dtype=torch.int32, device=self.dev)
+        self._step_buffers(bf, gamma)
+        lib = binding.load()
+        gemm_ws = max(lib.skinny_gemm_workspace_bytes(M, n, k) for n, k in
+                      ((qkv_n, s.hidden), (s.hidden, s.Hq * s.D), (2 * s.mlp, s.hidden), (s.hidden, s.mlp), (s.V, s.hidden)))
+        desc = binding.make_attn_desc(self.q_view, first["Kpre"], first["Kpriv"], self.attn)
+        self.ws_gemm = self._workspace(gemm_ws)
+        self.ws_attn = self._workspace(lib.verify_attention_workspace_bytes(ctypes.byref(desc)))
+        self.graph = None
+
+    def _workspace(self, n) -> torch.Tensor:
+        return torch.zeros(max(int(n), 256), dtype=torch.uint8, device=self.dev)
+
+    def _step_buffers(self, bf, gamma: int) -> None:
+        """The step's activations, what the acceptance reads and its results."""
+        s, B, R = self.s, self.B, self.R
+        M, qkv_n = B * R, (s.Hq + 2 * s.Hkv) * s.D
         z = lambda *sh: torch.zeros(sh, dtype=torch.bfloat16, device=self.dev)
         self.h = bf(M, s.hidden)
         self.qkv, self.attn, self.o, self.gu = z(M, qkv_n), z(B, R, s.Hq, s.D), z(M, s.hidden), z(M, 2 * s.mlp)
@@ -155,15 +172,7 @@ class FullModel:
         self.u = torch.full((B, R), 0.5, dtype=torch.float32, device=self.dev)
         self.accept_len = torch.zeros((B,), dtype=torch.int32, device=self.dev)
         self.next_token = torch.zeros((B,), dtype=torch.int32, device=self.dev)
-        lib = binding.load()
-        gemm_ws = max(lib.skinny_gemm_workspace_bytes(M, n, k) for n, k in
-                      ((qkv_n, s.hidden), (s.hidden, s.Hq * s.D), (2 * s.mlp, s.hidden), (s.hidden, s.mlp), (s.V, s.hidden)))
-        ws = lambda n: torch.zeros(max(int(n), 256), dtype=torch.uint8, device=self.dev)
-        desc = binding.make_attn_desc(self.q_view, first["Kpre"], first["Kpriv"], self.attn)
-        self.ws_gemm = ws(gemm_ws)
-        self.ws_attn = ws(lib.verify_attention_workspace_bytes(ctypes.byref(desc)))
-        self.ws_accept = ws(lib.spec_accept_logits_workspace_bytes(B, gamma, s.V))
-        self.graph = None
+        self.ws_accept = self._workspace(binding.load().spec_accept_logits_workspace_bytes(B, gamma, s.V))
 
     def enqueue(self) -> None:
         """One verify step of the whole stack on the current stream; allocates nothing."""
@@ -198,6 +207,70 @@ class FullModel:
         e1.record()
         torch.cuda.synchronize()
         return e0.elapsed_time(e1) / reps
+
+
+class MicroscaledModel(FullModel):
+    """FullModel with what a step streams held in microscaled numbers: the layers' weights in MXFP4, 4.25 bits each (17 GB for the 32B shape), and one paged
+    MXFP8 cache a layer, whose branches share the pages of the prefix.  A layer is the QKV projection, the append of its K and V columns, which quantises
+    them, verify_attention_paged_mxfp8, and the O, gate+up and down projections; the LM head stays in bf16."""
+
+    PAGE = 64
+
+    def __init__(self, shape: ModelShape, prefix: int, private: int, B: int, gamma: int, device="cuda:0"):
+        s, R, page = shape, gamma + 1, self.PAGE
+        M = B * R
+        if M > 256:
+            raise ValueError("one GEMM call takes at most 256 tokens")
+        self.s, self.B, self.R, self.dev = s, B, R, torch.device(device)
+        g = torch.Generator(device=self.dev)
+        g.manual_seed(11)
+        bf = lambda *sh: (torch.randn(*sh, generator=g, device=self.dev) * 0.5).to(torch.bfloat16)
+        w = lambda n, k: (torch.randn(n, k, generator=g, device=self.dev) * k ** -0.5).to(torch.bfloat16)
+        qkv_n = (s.Hq + 2 * s.Hkv) * s.D
+        shared, length = prefix // page, prefix + private + R
+        own = -(-length // page) - shared                      # pages of each branch; a prefix that ends inside a page has that page's rows in each
+        pages = shared + B * own
+        ids = torch.arange(pages, dtype=torch.int32, device=self.dev)
+        self.table = torch.cat([ids[:shared].expand(B, shared), ids[shared:].view(B, own)], 1).contiguous()
+        self.kv_len = torch.full((B,), length, dtype=torch.int32, device=self.dev)
+        codes = lambda last, dtype: torch.zeros((pages, s.Hkv, page, last), dtype=torch.uint8, device=self.dev).view(dtype)
+        first = {n: binding.mxfp4_quantize(w(*sh)) for n, sh in (("qkv", (qkv_n, s.hidden)), ("o", (s.hidden, s.Hq * s.D)), ("gate_up", (2 * s.mlp, s.hidden)),
+                                                                ("down", (s.hidden, s.mlp)))}
+        first["cache"] = tuple(codes(s.D, torch.float8_e4m3fn) for _ in "KV") + tuple(codes(s.D // 32, torch.float8_e8m0fnu) for _ in "KV")
+        fill = lambda table, new, lens: binding.kv_append_paged_mxfp8(bf(table.shape[0], new, s.Hkv, s.D), bf(table.shape[0], new, s.Hkv, s.D), *first["cache"],
+                                                                      table, lens)
+        if shared:                                             # once, through one branch's table
+            fill(self.table[:1], shared * page, torch.full((1,), shared * page, dtype=torch.int32, device=self.dev))
+        fill(self.table, length - shared * page, self.kv_len)
+        self.layers = [first] + [{k: tuple(t.clone() for t in v) for k, v in first.items()} for _ in range(s.layers - 1)]
+        self.lm_head = w(s.V, s.hidden)
+        self._step_buffers(bf, gamma)
+        heads = self.qkv.view(B, R, s.Hq + 2 * s.Hkv, s.D)
+        self.k_view, self.v_view = heads[:, :, s.Hq:s.Hq + s.Hkv], heads[:, :, s.Hq + s.Hkv:]
+        lib = binding.load()
+        self.ws_gemm = self._workspace(max([lib.skinny_gemm_workspace_bytes(M, s.V, s.hidden)] + [
+            lib.skinny_gemm_mxfp4_workspace_bytes(M, n, k) for n, k in
+            ((qkv_n, s.hidden), (s.hidden, s.Hq * s.D), (2 * s.mlp, s.hidden), (s.hidden, s.mlp))]))
+        desc = binding.PagedMxDesc(paged=binding.PagedDesc(B=B, T=M, max_new=R, Hq=s.Hq, Hkv=s.Hkv, D=s.D, page_tokens=page, pages=pages,
+                                                           columns=self.table.shape[1], dtype=binding.LOTTS_BF16))
+        self.ws_attn = self._workspace(lib.verify_attention_paged_mxfp8_workspace_bytes(ctypes.byref(desc)))
+        self.graph = None
+
+    def enqueue(self) -> None:
+        """One verify step of the whole stack on the current stream; allocates nothing."""
+        s, M = self.s, self.B * self.R
+        h = self.h
+        for L in self.layers:
+            binding.skinny_gemm_mxfp4(h, *L["qkv"], out=self.qkv, workspace=self.ws_gemm)
+            binding.kv_append_paged_mxfp8(self.k_view, self.v_view, *L["cache"], self.table, self.kv_len)
+            binding.verify_attention_paged_mxfp8(self.q_view, *L["cache"], self.table, self.kv_len, out=self.attn, workspace=self.ws_attn)
+            binding.skinny_gemm_mxfp4(self.attn.view(M, s.Hq * s.D), *L["o"], out=self.o, workspace=self.ws_gemm)
+            binding.skinny_gemm_mxfp4(self.o, *L["gate_up"], out=self.gu, workspace=self.ws_gemm)
+            binding.skinny_gemm_mxfp4(self.gu[:, :s.mlp], *L["down"], out=self.o, workspace=self.ws_gemm)
+            h = self.o
+        binding.skinny_gemm(h, self.lm_head, out=self.zt.view(M, s.V), workspace=self.ws_gemm)
+        binding.spec_accept_logits(self.zt, self.zd, self.draft, self.u, accept_len=self.accept_len,
+                                   next_token=self.next_token, workspace=self.ws_accept)
 
 
 def expected_tokens_per_step(alpha: float, gamma: int) -> float:
@@ -269,6 +342,8 @@ def main() -> int:
     ap.add_argument("--full-model", metavar="B,GAMMA", action="append", default=[],
                     help="also hold every layer of the shape on the GPU and time one verify step of the whole stack "
                          "for this (B, gamma), against the sum of isolated kernel times the search uses")
+    ap.add_argument("--microscaled", action="store_true",
+                    help="also time that step with the weights in MXFP4 and a paged cache in MXFP8")
     a = ap.parse_args()
     for spec in a.full_model:
         B, gamma = (int(x) for x in spec.split(","))
@@ -278,10 +353,16 @@ def main() -> int:
         measured = fm.step_ms()
         del fm
         torch.cuda.empty_cache()
+        microscaled = {}
+        if a.microscaled:
+            fm = MicroscaledModel(SHAPES[a.shape], prefix, private, B, gamma)
+            microscaled["step_ms_whole_stack_mxfp4_weights_mxfp8_cache"] = fm.step_ms()
+            del fm
+            torch.cuda.empty_cache()
         modelled = StepTimer(SHAPES[a.shape], prefix, context, B, gamma).verify_step_ms(B, gamma, private)
         print(json.dumps({"full_model": SHAPES[a.shape].name, "B": B, "gamma": gamma, "private_tokens": private,
                           "step_ms_whole_stack_graph_replay": measured, "step_ms_sum_of_kernel_times": modelled["total"],
-                          "per_layer_ms_sum_of_kernel_times": modelled["layer"]}), flush=True)
+                          "per_layer_ms_sum_of_kernel_times": modelled["layer"], **microscaled}), flush=True)
     if a.budget_s <= 0.0:  # only the whole-stack measurements were asked for
         return 0
     out = search(a.shape, a.budget_s, alpha=a.alpha, draft_ratio=a.draft_ratio, B_max=a.B_max, gamma_max=a.gamma_max,

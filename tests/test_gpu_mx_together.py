@@ -124,3 +124,54 @@ def test_a_projection_larger_than_the_step(lotts):
     exact, off = a @ w.t(), (Hq * D + 64) * 2.0 ** -23 * (a.abs() @ w.abs().t())
     assert ((Y.cpu().double() - exact).abs() <= off + 2.0 ** -8 * (exact.abs() + off)).all()
     assert math.isfinite(float(Y.float().abs().max()))
+
+
+def test_the_whole_stack_step_of_the_latency_model(lotts):
+    """Two layers of a tiny decoder with MXFP4 weights and a paged MXFP8 cache, a prefix that ends inside a page: the last layer's products and attention against 64
+    bits from what went into them, and replays of the captured step against the eager one, bit for bit."""
+    from mx_util import unpack
+    from paper_2505_19634_amd import latency_model as lm
+    shape = lm.ModelShape("tiny decoder", 2, 512, 8, 2, 64, 1024, 4096)
+    B, R, prefix, private = 4, 3, 150, 70
+    fm = lm.MicroscaledModel(shape, prefix, private, B, R - 1)
+    fm.enqueue()
+    torch.cuda.synchronize()
+    results = (fm.qkv, fm.attn, fm.gu, fm.o, fm.zt, fm.accept_len, fm.next_token) + fm.layers[0]["cache"] + fm.layers[1]["cache"]
+    raw = lambda t: t.view(torch.uint8) if t.dtype in (torch.float8_e4m3fn, torch.float8_e8m0fnu) else t
+    want = [raw(t).clone() for t in results]
+    last, w64 = fm.layers[1], lambda pair: torch.from_numpy(values(unpack(pair[0].cpu().numpy()), raw(pair[1]).cpu().numpy(), "mxfp4"))
+
+    def product(x, pair, got):
+        x, w = x.cpu().double(), w64(pair)
+        exact, off = x @ w.t(), (x.shape[1] + 64) * 2.0 ** -23 * (x.abs() @ w.abs().t())
+        assert ((got.cpu().double() - exact).abs() <= off + 2.0 ** -8 * (exact.abs() + off)).all()
+    a = fm.attn.view(B * R, -1)
+    o = torch.empty_like(fm.o)
+    lotts.skinny_gemm_mxfp4(a, *last["o"], out=o, workspace=fm.ws_gemm)
+    product(a, last["o"], o)
+    product(o, last["gate_up"], fm.gu)
+    product(fm.gu[:, :shape.mlp], last["down"], fm.o)
+    # the cache: the pages of the prefix are shared, the rest is each branch's own, the last rows are the step's
+    L, page = prefix + private + R, fm.PAGE
+    table = fm.table.cpu()
+    assert (table[:, :prefix // page] == table[0, :prefix // page]).all() and len(set(table[:, prefix // page:].flatten().tolist())) == table[:, prefix // page:].numel()
+    c = P.Cache([R] * B, [L] * B, shape.Hq, shape.Hkv, shape.D, page, device="cpu")
+    held = [torch.from_numpy(values(raw(x).cpu().numpy(), raw(y).cpu().numpy(), "mxfp8")) for x, y in zip(last["cache"][:2], last["cache"][2:])]
+    c.k, c.v = ([h[table[b].long()].transpose(1, 2).reshape(-1, shape.Hkv, shape.D)[:L] for b in range(B)] for h in held)
+    heads = fm.qkv.cpu().view(B * R, -1, shape.D)
+    new = torch.from_numpy(values(*quantise(heads[:, shape.Hq:].float(), "mxfp8"), "mxfp8")).view(B, R, 2, shape.Hkv, shape.D)
+    for b in range(B):
+        assert torch.equal(c.k[b][-R:], new[b, :, 0]) and torch.equal(c.v[b][-R:], new[b, :, 1])
+    c.q = heads[:, :shape.Hq]
+    P.check(c, fm.attn.view(B * R, shape.Hq, shape.D))
+    for t in results[:5]:
+        t.zero_()
+    assert fm.step_ms(reps=3) > 0.0
+    for turn in range(2):
+        for got, was in zip(results, want):
+            assert torch.equal(raw(got), was)
+        fm.attn.zero_()
+        fm.graph.replay()
+        torch.cuda.synchronize()
+    with pytest.raises(ValueError):
+        lm.MicroscaledModel(shape, 64, 64, 100, 2)
