@@ -33,7 +33,7 @@ constexpr int kWideRows = 256;       // rows of a wide item
 // kept some workgroups 34 us and others 68.)
 constexpr int kNarrowCost = 2, kStartCost = 6;
 constexpr int wide_cost(int D) { return D == 64 ? 9 : 7; }
-constexpr int kMaxWideCost = 9;
+constexpr int kMaxKeyCost = 9;       // places of 32 keys, at most
 // Places of a worker below which there are no more workers than items, and for narrow items that take more than this on average: 4 tiles, one for each
 // wavefront.  (With 32 for both: 16 branches of 512 tokens 22.6 us against 13.2, 64 of 700 22.6 against 16.0, one of 2000 17.4 against 10.6; 2 tiles are
 // no faster; with 8 for both one branch of 300 tokens 9.2 against 8.3.)  A cut of a wide item moves 256 rows.
@@ -72,6 +72,13 @@ struct PagedMxParams : PagedParams {
 
 template <typename P>
 constexpr bool kMx = std::is_same<P, PagedMxParams>::value;
+// An MXFP8 cache's: a narrow tile is half of the bytes, 0.2 and 0.3 us, a wide one's codes are converted on their way, 1.5 and 2.2, and a start in a call that has both
+// 2 to 3.  (At the costs above, 31 branches of up to 4000 tokens beside a chunk of 500, 40 / 8 heads, D = 128: 125 us, here 101; 32 / 8 heads, D = 64: 74 and 66;
+// 63 of 3000 beside 2048, 198 and 173; starts at 6 180.  Wide tiles at 20: 98, 66, 183.)
+template <typename P>
+constexpr int wide_cost(int D) { return !kMx<P> ? wide_cost(D) : D == 64 ? 15 : 14; }
+template <typename P, bool WIDE>
+constexpr int start_cost() { return kMx<P> && WIDE ? 20 : kStartCost; }
 
 // A branch of the call: its first row of Q, its new tokens and all its tokens (both brought into the range that the arguments allow, so
 // that nothing is addressed out of bounds whatever the device data say).
@@ -142,8 +149,8 @@ __device__ __forceinline__ int first_slot(const PagedParams& p, int b) {
     const int first = p.q_start ? min(max(p.q_start[b], 0), p.T) : b * p.R;
     return (int)((long long)first * p.G / kWideRows) + b;
 }
-template <int D, bool WIDE, int NARROW_TILES>
-__device__ __forceinline__ Items items_at(const PagedParams& p, int base, unsigned before, int lane) {
+template <int D, bool WIDE, int NARROW_TILES, typename P>
+__device__ __forceinline__ Items items_at(const P& p, int base, unsigned before, int lane) {
     const int slot = base + lane;
     Items t;
     int b = min(slot, p.B - 1);
@@ -166,7 +173,7 @@ __device__ __forceinline__ Items items_at(const PagedParams& p, int base, unsign
     const int keys = max(1, br.L - br.n + quot(max(end, 1) - 1, p.d_g) + 1);
     t.b = b; t.first = br.first; t.n = br.n; t.L = br.L;
     t.tiles = narrow ? (keys - 1) / kNarrowTile + 1 : (keys - 1) / kWideTile + 1;
-    t.cost = there ? kStartCost + t.tiles * (narrow ? kNarrowCost : wide_cost(D)) : 0;
+    t.cost = there ? start_cost<P, WIDE>() + t.tiles * (narrow ? kNarrowCost : wide_cost<P>(D)) : 0;
     t.end = before + wave_incl_scan_u32((unsigned)t.cost);
     return t;
 }
@@ -1183,7 +1190,7 @@ __global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave)
     __shared__ __attribute__((aligned(16))) int sh_first[WAVES][D];
     const int lane = threadIdx.x & (kWave - 1);
     const int per_xcd = p.workers / kNumXCD;  // neighbours in the sequence share an XCD and with it a KV head's keys in its L2
-    const int w = (int)(blockIdx.x % kNumXCD) * per_xcd + (int)(blockIdx.x / kNumXCD);
+    int w = (int)(blockIdx.x % kNumXCD) * per_xcd + (int)(blockIdx.x / kNumXCD);
     int base = 0;
     Items items = items_at<D, WIDE, NARROW_TILES>(p, 0, 0, lane);
     unsigned total = __builtin_amdgcn_readlane(items.end, kWave - 1);
@@ -1195,7 +1202,7 @@ __global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave)
     }
     if (total == 0) return;
     // Every piece has at least one tile of an item that it lies in: whoever counts an item's parts counts on that.
-    constexpr int LEAST = WIDE ? kMaxWideCost + 1 : kNarrowCost + 2;
+    constexpr int LEAST = WIDE ? (kMx<P> ? wide_cost<P>(D) : wide_cost(64)) + 1 : kNarrowCost + 2;
     Pieces pieces;
     pieces.places = (double)total * p.Hkv;
     const double all = (double)number * p.Hkv;  // items
@@ -1211,11 +1218,11 @@ __global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave)
     double size = 0.0;
     unsigned parts_total = 0;
     auto parts_of = [&](Items& t, unsigned before) {
-        t.cost = t.cost > 0 ? max(1, (int)ceil((t.cost - kStartCost) / size)) : 0;
+        t.cost = t.cost > 0 ? max(1, (int)ceil((t.cost - start_cost<P, WIDE>()) / size)) : 0;
         t.end = before + wave_incl_scan_u32((unsigned)t.cost);
     };
-    if (WIDE && all <= 0.75 * p.workers && pieces.places < kApartPlaces * (double)p.workers) {
-        size = fmax(1.0, (pieces.places - all * kStartCost) / (p.workers - 0.6 * all));
+    if (WIDE && all <= 0.75 * p.workers && pieces.places < (double)kApartPlaces * wide_cost<P>(D) / wide_cost(D) * p.workers) {
+        size = fmax(1.0, (pieces.places - all * start_cost<P, WIDE>()) / (p.workers - 0.6 * all));
         for (int s = 0; s < p.items; s += kWave) {
             Items more = items;
             if (s > 0) more = items_at<D, WIDE, NARROW_TILES>(p, s, 0, lane);
@@ -1231,6 +1238,16 @@ __global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave)
         at = w;
         end = (long long)total * p.Hkv;
     } else {
+        if constexpr (kMx<P>) {
+            // Two heads' rows of 64 bytes lie in one line: their workers alternate on an XCD, so that its L2 fetches the line once.  (31 branches of 16000 tokens,
+            // 32 / 8 heads, tokens in front of heads: 171 -> 128 us; 16 / 16 heads, whose workers lie so already, 293.  All heads alternating, for the lines that
+            // their scales share: 126, but branches that share a prefix miss it in the L2: 64 of 8192 with 7000 in common 106 -> 111, here 99.)
+            if (D == 64 && p.page_h == D && p.Hkv % 2 == 0 && pieces.workers >= 4 * p.Hkv) {
+                const int each = pieces.workers / p.Hkv, r = w % (2 * each);
+                pieces.workers = each * p.Hkv;
+                w = w < pieces.workers ? w - r + (r & 1) * each + (r >> 1) : w;
+            }
+        }
         if (w >= pieces.workers) return;
         at = pieces.start(w);
         end = pieces.start(w + 1);
@@ -1269,8 +1286,8 @@ __global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave)
             g.slot_step = 1;
             at += p.workers;
         } else {
-            const int each = narrow ? kNarrowCost : wide_cost(D);
-            const long long tile0 = head + item_end - cost + kStartCost;
+            const int each = narrow ? kNarrowCost : wide_cost<P>(D);
+            const long long tile0 = head + item_end - cost + start_cost<P, WIDE>();
             auto tile_from = [&](long long place) { return place <= tile0 ? 0 : (int)min((long long)g.tiles, (place - tile0 + each - 1) / each); };
             g.lo = tile_from(at);
             g.hi = tile_from(end);
@@ -1444,7 +1461,8 @@ static int paged_desc(const lotts_paged_desc* in, bool uniform, bool mx, lotts_p
     if (d->page_stride_t * cache_es > (1LL << 26)) return LOTTS_ERR_SHAPE;  // 16 keys of a page: 32-bit offsets
     // the sequence of work of a KV head in 32 bits (were every branch as long as the table allows)
     const long long G = d->Hq / d->Hkv, slots = (long long)d->T * G / kWideRows + d->B;
-    if (((long long)d->columns << *shift) / kNarrowTile * kMaxWideCost + kMaxWideCost + kStartCost > 0x7fffffffLL / slots) return LOTTS_ERR_SHAPE;
+    // (a key's places are at most 15 / 64 of a wide tile; a last tile's and the start's are 15 and 20 more)
+    if (((long long)d->columns << *shift) / kNarrowTile * kMaxKeyCost + (mx ? 40 : kMaxKeyCost + kStartCost) > 0x7fffffffLL / slots) return LOTTS_ERR_SHAPE;
     if ((long long)d->T * d->Hq >= (1LL << 24)) return LOTTS_ERR_SHAPE;  // a grid holds fewer than 2^24 workgroups of 256 threads
     return LOTTS_OK;
 }
