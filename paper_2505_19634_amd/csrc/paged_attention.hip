@@ -528,17 +528,20 @@ struct NotFinite {
 // on its way to the products: a lane has a key's row there and takes 16 codes at a time, so the two products behind them have 8 each, and Q's fragments are
 // chosen to match.  What a product multiplies with what in which of its places does not matter.  Everything of a tile has been read from LDS before its products,
 // and the next one is on its way under them.
-template <typename P, int D, int TW, int WAVES, int STAGES>
+// RG = 2: two groups of wavefronts with a row tile each, instead of TW = 2.
+template <typename P, int D, int TW, int WAVES, int STAGES, int RG = 1>
 __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, unsigned char* lds, float (*sh_m)[32], float (*sh_l)[32], int* sh_bad, int (*sh_first)[D], int* sh) {
     using X = Tile<D>;
     constexpr bool MX = kMx<P>;
+    constexpr int KW = WAVES / RG;  // wavefronts that share a row tile's keys out
+    static_assert(RG == 1 || TW == 1, "row tiles lie beside each other in a wavefront or in wavefronts");
     constexpr int ROW = D * 2, HALF = kNarrowTile * ROW, SLAB = narrow_slab<D>(STAGES), LOADS = 4 * X::NLD;  // of a tile
     constexpr int CODES = kNarrowTile * D, LPR = MX ? D / 16 : X::LPR, RPI = kWave / LPR, NLD = kPgGroup / RPI;  // an MXFP8 slab: K's codes, V's, V
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid & (kWave - 1);
-    const int ln = lane & 31, hh = lane >> 5;
+    const int ln = lane & 31, hh = lane >> 5, wk = RG > 1 ? wave % KW : wave, row_from = RG > 1 ? wave / KW * 32 : 0;
     const int32_t* row = p.table + g.b * p.table_stride;
     const int keys = min(g.L, max(0, g.L - g.n + quot(g.nrows - 1, p.d_g) + 1)), before = g.L - g.n;
-    const int n_tiles = g.lo + wave < g.hi ? (g.hi - 1 - g.lo - wave) / WAVES + 1 : 0;
+    const int n_tiles = g.lo + wk < g.hi ? (g.hi - 1 - g.lo - wk) / KW + 1 : 0;
     const int v_row = lane / LPR, v_slot = lane % LPR;
     const unsigned slab = lds_address(lds) + wave * SLAB, row_off = (unsigned)v_row * (unsigned)p.page_t;
     const unsigned piece = (v_slot ^ (MX ? spread_codes<D>(v_row) : spread<D>(v_row))) * 16;  // of the first load; the others' differ in the bits that spread() takes from the row's upper part
@@ -551,7 +554,7 @@ __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, uns
         ahead_from = it;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int key = (g.lo + wave + (it + lane) * WAVES) * kNarrowTile + h * kPgGroup, e = page_entry(p, row, key);
+            const int key = (g.lo + wk + (it + lane) * KW) * kNarrowTile + h * kPgGroup, e = page_entry(p, row, key);
             const long long at = group_at(p, e, key, g.kvh);
             ahead_lo[h] = (unsigned)at;
             ahead_hi[h] = (unsigned)(at >> 32);
@@ -575,7 +578,7 @@ __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, uns
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 at[h] = (unsigned long long)(unsigned)__builtin_amdgcn_readlane(ahead_scale_hi[h], x) << 32 | (unsigned)__builtin_amdgcn_readlane(ahead_scale_lo[h], x);
-                n[h] = __builtin_amdgcn_readlane(ahead_bytes[h], x) & ~1 ? keys - (g.lo + wave + it * WAVES) * kNarrowTile - h * kPgGroup : 0;
+                n[h] = __builtin_amdgcn_readlane(ahead_bytes[h], x) & ~1 ? keys - (g.lo + wk + it * KW) * kNarrowTile - h * kPgGroup : 0;
             }
             const unsigned char* from = (hh ? p.Vs : p.Ks) + (long long)(group ? at[1] : at[0]) + (unsigned)r * (unsigned)p.scale_t;
             next_scales = 0;
@@ -590,8 +593,8 @@ __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, uns
 #pragma unroll
             for (int i = 0; i < NLD; ++i) {
                 const unsigned off = row_off + (unsigned)(i * RPI) * (unsigned)p.page_t + (piece ^ (MX ? spread_codes<D>(i * RPI) : spread<D>(i * RPI)) * 16);
-                load_to_lds<true>(kr, off, stage + h * kPgGroup * (MX ? D : ROW) + i * 1024);
-                load_to_lds<true>(vr, off, stage + (MX ? CODES : HALF) + h * kPgGroup * (MX ? D : ROW) + i * 1024);
+                load_to_lds<RG == 1>(kr, off, stage + h * kPgGroup * (MX ? D : ROW) + i * 1024);
+                load_to_lds<RG == 1>(vr, off, stage + (MX ? CODES : HALF) + h * kPgGroup * (MX ? D : ROW) + i * 1024);
             }
         }
         return have;
@@ -605,7 +608,7 @@ __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, uns
     int lim[TW];
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
-        const int r = min(t * 32 + ln, g.nrows - 1), i = quot(r, p.d_g);
+        const int r = min(row_from + t * 32 + ln, g.nrows - 1), i = quot(r, p.d_g);
         lim[t] = before + i + 1;
         const unsigned char* qp = (const unsigned char*)p.Q + (long long)(g.first + i) * p.q_t + (g.kvh * p.G + r - i * p.G) * p.q_h;
 #pragma unroll
@@ -629,7 +632,7 @@ __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, uns
             for (int i = 0; i < 16; ++i) oacc[t][db][i] = 0.f;
     }
     for (int it = 0; it < n_tiles; ++it) {
-        const int kb = (g.lo + wave + it * WAVES) * kNarrowTile, have = have_next;
+        const int kb = (g.lo + wk + it * KW) * kNarrowTile, have = have_next;
         const unsigned stage = STAGES > 1 ? (it & 1) * 2 * HALF : 0;
         bf16x8 kf[X::KS], pf[TW][2];
         if constexpr (MX) {
@@ -695,7 +698,7 @@ __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, uns
         NotFinite<D> bad;
 #pragma unroll 1
         for (int it = 0; it < n_tiles; ++it) {
-            const int kb = (g.lo + wave + it * WAVES) * kNarrowTile;
+            const int kb = (g.lo + wk + it * KW) * kNarrowTile;
             bad.look(p, row, g.kvh, max(kb, unseen), min(kb + kNarrowTile, keys));
         }
         bad.publish(lds_address(sh_first[wave]));
@@ -724,16 +727,16 @@ __device__ __forceinline__ void narrow_segment(const P& p, const Segment& g, uns
         __syncthreads();
         const bool any_bad = __ballot(sh_bad[lane % WAVES] != 0) != 0;
 #pragma unroll
-        for (int q = 0; q < QPT; ++q) {
-            const int rt = row0 + q * RSTEP, r = t * 32 + rt;
+        for (int q = 0; q < RG * QPT; ++q) {
+            const int rt = row0 + q % QPT * RSTEP, from = q / QPT * KW, r = (t + q / QPT) * 32 + rt;
             if (r >= g.nrows) continue;
             float M = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int v = 0; v < WAVES; ++v) M = fmaxf(M, sh_m[v][rt]);
+            for (int v = from; v < from + KW; ++v) M = fmaxf(M, sh_m[v][rt]);
             const float Mu = M == -INFINITY ? 0.f : M;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int v = 0; v < WAVES; ++v) {
+            for (int v = from; v < from + KW; ++v) {
                 const float f = __builtin_amdgcn_exp2f((sh_m[v][rt] - Mu) * p.scale_log2);
                 const float4 ov = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds + v * SLAB) + rt * X::OSTRIDE + c4 * 4);
                 sum += sh_l[v][rt] * f;
@@ -1175,10 +1178,11 @@ __device__ __forceinline__ void wide_segment(const P& p, const Segment& g, unsig
     __syncthreads();
 }
 
-// Wavefronts of a workgroup.  (Of an MXFP8 cache a tile is half as many bytes: eight have as much on the way as four with two slabs each.)
+// Wavefronts of a workgroup.  (Of an MXFP8 cache a tile is half as many bytes: eight have as much on the way as four with two slabs each.  16 branches of 4096, 8
+// heads, D = 128, 20 rows each 42.8 -> 31.0 us; D = 64, 36 rows 39 -> 28.)
 template <typename P, int NARROW_TILES, bool WIDE, bool TWO>
 __host__ __device__ constexpr int paged_waves() {
-    return WIDE || (kMx<P> && NARROW_TILES == 1 && !TWO) ? 8 : 4;
+    return WIDE || (kMx<P> && !TWO) ? 8 : 4;
 }
 template <typename P, int D, int NARROW_TILES, bool WIDE, bool TWO>
 __global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave), TWO || WIDE ? 2 : 1) void paged_attn_kernel(const P p) {
@@ -1310,6 +1314,12 @@ __global__ __launch_bounds__((paged_waves<P, NARROW_TILES, WIDE, TWO>() * kWave)
         if constexpr (WIDE) {
             if (narrow) narrow_segment<P, D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
             else wide_segment<P, D, WAVES>(p, g, lds, &sh, sh_bad);
+        } else if constexpr (kMx<P> && D == 128 && NARROW_TILES > 1) {
+            // Eight wavefronts have no registers for two row tiles each: there four take each.  A key tile is read twice, the second time from the L2 (past it, as
+            // what is read once: 52.7).  16 branches of 4096 with 7 new tokens, 40 / 8 heads, 47.5 us, with four wavefronts of two row tiles 54.3, eight, which
+            // spill, 102; one of 2000 with 5, 16 / 2 heads, 17.7, 22.8, 34.
+            if (g.nrows > 32) narrow_segment<P, D, 1, WAVES, STAGES, 2>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
+            else narrow_segment<P, D, 1, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
         } else {
             narrow_segment<P, D, NARROW_TILES, WAVES, STAGES>(p, g, lds, sh_m, sh_l, sh_bad, sh_first, &sh);
         }
