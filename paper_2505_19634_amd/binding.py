@@ -621,10 +621,11 @@ def mxfp4_quantize(W: torch.Tensor, *, codes: Optional[torch.Tensor] = None, sca
     device = _current_gpu("mxfp4_quantize", W)
     if W.dim() != 2:
         raise ValueError("the matrix must be [N][K] with contiguous rows")
+    N, K = W.shape
     if codes is None:
-        codes = torch.empty((W.shape[0], W.shape[1] // 2), dtype=torch.uint8, device=W.device)
+        codes = W.new_empty((N, K // 2), dtype=torch.uint8)
     if scales is None:
-        scales = torch.empty((W.shape[0], W.shape[1] // 32), dtype=torch.float8_e8m0fnu, device=W.device)
+        scales = W.new_empty((N, K // 32), dtype=torch.float8_e8m0fnu)
     rc = lib.mx.mxfp4_quantize(W, codes, scales, device, _stream_handle(stream))
     if rc != 0:
         raise LottsError(rc, "mxfp4_quantize")
@@ -639,7 +640,8 @@ def mxfp4_dequantize(codes: torch.Tensor, scales: torch.Tensor, *, dtype: torch.
     if codes.dim() != 2:
         raise ValueError("codes must be [N][K / 2] with contiguous rows")
     if out is None:
-        out = torch.empty((codes.shape[0], 2 * codes.shape[1]), dtype=dtype, device=codes.device)
+        N, pairs = codes.shape
+        out = codes.new_empty((N, 2 * pairs), dtype=dtype)
     rc = lib.mx.mxfp4_dequantize(out, codes, scales, device, _stream_handle(stream))
     if rc != 0:
         raise LottsError(rc, "mxfp4_dequantize")

@@ -159,3 +159,68 @@ def test_weights_beyond_4_gib(lotts):
     out = lotts.skinny_gemm_mxfp4(p.X, codes, scales)
     p.check(out[:, -300:])
     assert (out[:, :-300] == 0).all()
+
+
+# Sizes at which each of the ways to cut the work is taken, with K's last chunk whole and not, K in one piece and in several; tokens and rows that fill no tile.
+FORMS = [(20, 20000, 1056), (20, 20003, 512), (1, 40, 11040), (1, 40, 8192), (32, 9000, 1056), (1, 9001, 2048), (1, 1024, 11040), (3, 40, 16384),
+         (33, 20000, 1056), (33, 20001, 512), (33, 40, 5152), (40, 41, 4096), (33, 9000, 2080), (64, 5000, 2048), (33, 5000, 2080), (63, 40, 16384),
+         (70, 20000, 256), (70, 20001, 288), (96, 20000, 512), (70, 40, 5152), (70, 43, 4096), (100, 20000, 160), (100, 20000, 256), (100, 20000, 288),
+         (128, 9000, 512), (100, 40, 5152), (127, 40, 5120), (130, 20000, 160), (131, 20002, 256), (130, 40, 11040), (191, 300, 8192), (256, 20000, 64),
+         (200, 20000, 256), (200, 40, 11040), (201, 40, 9600), (256, 5120, 5120), (31, 55301, 1056), (31, 55300, 1280), (64, 55301, 1056), (64, 55297, 1280),
+         (96, 55299, 1056), (96, 55300, 1280), (128, 55301, 1056), (128, 55300, 1280), (255, 55301, 1056), (255, 55300, 1280)]
+
+
+class OnDevice:
+    """Any codes, scales over a few powers of two; the reference is a product in 64 bits of what these stand for."""
+
+    def __init__(self, M, N, K, ldx=None, ld_codes=None, ld_scales=None):
+        g = torch.Generator(device=DEV).manual_seed(M + N + K)
+        rows = lambda n, k, ld, dtype: torch.empty(n * (ld or k), dtype=dtype, device=DEV).view(n, ld or k)[:, :k]
+        self.X, self.codes, self.scales = rows(M, K, ldx, torch.bfloat16), rows(N, K // 2, ld_codes, torch.uint8), rows(N, K // 32, ld_scales, torch.uint8)
+        self.X.copy_(torch.randn(M, K, generator=g, device=DEV))
+        self.codes.copy_(torch.randint(0, 256, self.codes.shape, generator=g, device=DEV, dtype=torch.uint8))
+        self.scales.copy_(torch.randint(118, 124, self.scales.shape, generator=g, device=DEV, dtype=torch.uint8))
+
+    def check(self, lotts, got):
+        x, w = self.X.double(), lotts.mxfp4_dequantize(self.codes, self.scales, dtype=torch.float32).double()
+        Y = x @ w.t()
+        off = (x.shape[1] + 64) * 2.0 ** -23 * (x.abs() @ w.abs().t())
+        assert ((got.double() - Y).abs() <= off + 2.0 ** -8 * (Y.abs() + off)).all()
+
+
+@pytest.mark.parametrize("M,N,K", FORMS)
+def test_every_cut(lotts, M, N, K):
+    print("mxfp4 product", M, N, K, flush=True)
+    p = OnDevice(M, N, K)
+    out = torch.full((M, N + 3), 7.0, dtype=torch.bfloat16, device=DEV)
+    p.check(lotts, lotts.skinny_gemm_mxfp4(p.X, p.codes, p.scales, out=out[:, :N]))
+    assert (out[:, N:] == 7).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(256, 600, 16384), (100, 600, 16384), (20, 300, 16384), (3, 60, 512)])
+def test_the_widest_pitches(lotts, M, N, K):
+    """Rows of codes and scales 16 MiB apart, tokens 8 MiB: the last row of a workgroup lies 2^30 bytes and more behind its first."""
+    print("mxfp4 product, widest pitches", M, N, K, flush=True)
+    p = OnDevice(M, N, K, 1 << 22, 1 << 24, 1 << 24)
+    p.check(lotts, lotts.skinny_gemm_mxfp4(p.X, p.codes, p.scales))
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 300, 96), (20, 20000, 1056), (1, 1024, 11040), (33, 40, 5152), (64, 9001, 2080), (70, 40, 5152), (100, 20000, 288), (130, 40, 11040),
+                                   (200, 20000, 288), (256, 600, 16384)])
+def test_what_lies_behind_rows_and_what_is_no_number(lotts, M, N, K):
+    """NaN between the rows and behind the last one reaches nothing; a token's NaN reaches that token's row, a weight's that weight's column."""
+    print("mxfp4 product, NaN", M, N, K, flush=True)
+    p = OnDevice(M + 1, N + 1, K, K + 64, K // 2 + 32, K // 32 + 4)
+    whole = lambda t, ld: t.as_strided((t.shape[0], ld), (ld, 1))
+    X, codes, scales = p.X[:M].clone(), p.codes[:N].clone(), p.scales[:N].clone()
+    whole(p.X, K + 64).fill_(math.nan)
+    whole(p.scales, K // 32 + 4).fill_(255)
+    p.X, p.codes, p.scales = p.X[:M].copy_(X), p.codes[:N].copy_(codes), p.scales[:N].copy_(scales)
+    clean = lotts.skinny_gemm_mxfp4(p.X, p.codes, p.scales)
+    p.check(lotts, clean)
+    m, n = M // 2, N // 3
+    p.X[m, K - 1], p.scales[n, 0] = math.nan, 255
+    got = lotts.skinny_gemm_mxfp4(p.X, p.codes, p.scales)
+    bad = torch.zeros(M, N, dtype=torch.bool, device=DEV)
+    bad[m], bad[:, n] = True, True
+    assert torch.equal(got.isnan(), bad) and torch.equal(got[~bad], clean[~bad])
