@@ -367,3 +367,49 @@ def test_device_data_outside_the_contract(lotts, dtype):
         for starts in ([0, 40, 2, 4, 9, 49], [5, 3, 1, 0, 0, 0], [-9, -2, 20, 90, 3, 1], [100, 200, 300, 400, 500, 600], [0, 2 ** 31 - 1, -2 ** 31, 7, 8, 9], [2] * 6):
             attend_(torch.tensor(starts, dtype=torch.int32, device=DEV), c.kv_len, max_new)
         assert ((attend_(c.q_start, c.kv_len, max_new) - O).abs() <= tol).all()   # the workspace serves the next call
+
+
+BETWEEN = [(8, 3000), (5, 700), (1, 100), (6, 6), (7, 33), (4, 200), (0, 50), (8, 3), (3, 4000)]   # of 8 heads a KV head: up to 64 rows
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,layout,page", [(16, 2, 128, "head", 16), (8, 1, 128, "token", 64), (64, 8, 128, "head", 32), (16, 2, 64, "token", 16), (7, 1, 128, "head", 64)])
+@pytest.mark.parametrize("holes", [False, True])
+def test_up_to_64_rows_of_a_branch(lotts, Hq, Hkv, D, layout, page, holes):
+    """Items of up to 32 and of up to 64 rows in a call, in one piece and cut."""
+    new, length = zip(*BETWEEN)
+    gone = [(0, 0, -1), (1, 2, 5), (8, 100 * 16 // page, -1), (3, 0, -7)] if holes else ()
+    c = MxCache(new, length, Hq, Hkv, D, page, "bf16", layout, holes=gone, seed=Hq + D)
+    check(c, *attend(lotts, c, max_new=8))
+    first = attend(lotts, c, max_new=8)
+    for a, b in zip(first, attend(lotts, c, max_new=8)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,page,layout", [(16, 2, 128, 16, "head"), (40, 5, 128, 32, "token"), (16, 2, 64, 16, "token")])
+def test_nan_in_v_of_up_to_64_rows(lotts, Hq, Hkv, D, page, layout):
+    """A block of NaN in V at keys that some of the new tokens see and some do not."""
+    new, length = zip(*BETWEEN)
+    c = MxCache(new, length, Hq, Hkv, D, page, "bf16", layout, seed=D)
+    scales, off = c.Vs.view(torch.uint8), torch.zeros(c.q.shape, dtype=torch.bool)
+    for b, (n, L) in enumerate(BETWEEN):
+        first = L - n
+        for i, key in enumerate(range(max(first, 0), L, 2)):
+            h, block = i % Hkv, i % (D // 32)
+            scales[int(c.table[b, key // page]), h, key % page, block] = 255
+            c.v[b][key, h, block * 32:block * 32 + 32] = 0.0
+            off[c.starts[b] + key - first:c.starts[b] + n, h * (Hq // Hkv):(h + 1) * (Hq // Hkv), block * 32:block * 32 + 32] = True
+    O, _, tol, _ = c.reference()
+    got = lotts.verify_attention_paged_mxfp8(c.Q, *c.cache, c.table, c.kv_len, c.q_start, max_new=8).cpu().double()
+    assert torch.isnan(got[off]).all() and ((got - O).abs() <= tol)[~off].all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,page,most", [(32, 8, 32, 2), (8, 2, 16, 4), (12, 6, 64, 3), (16, 16, 16, 1), (32, 8, 16, 300)])
+def test_heads_of_64_next_to_each_other(lotts, Hq, Hkv, page, most):
+    """Tokens in front of heads: two heads' codes of a key lie in one line of memory, and their workers alternate.  Branches of all lengths, a few and many."""
+    for B in (1, 9, 70):
+        new = [1 + i % min(most, 4) for i in range(B)]
+        if most > 4:
+            new[B // 2] = most
+        length = [n + (i * 911) % 1500 for i, n in enumerate(new)]
+        c = MxCache(new, length, Hq, Hkv, 64, page, "bf16", "token", seed=B + Hq)
+        check(c, *attend(lotts, c, max_new=max(new)))
