@@ -800,10 +800,10 @@ __device__ __forceinline__ void mfma_done(f32x16 (&d)[N]) {
 // that nothing in a slot depends on anything else in it; scheduling barriers keep the slots apart.  Loads go out a few a step: all of a tile's at
 // once held the wavefronts 1000 to 1600 cycles a tile.  (4 wavefronts of two row tiles, a SIMD each: a prompt of 2039 tokens,
 // 16 / 2 heads, 81 us against 62 with 8; 2 chunks of 2048 alike.)
-// LOADS: what a wavefront requests of a tile's K and V in the slots (of an MXFP8 cache nothing: arrive() does).
-template <int D, int LOADS, typename Arrive, typename Request>
+// LOADS: what a wavefront requests of a tile's K and V in the slots (of an MXFP8 cache nothing: arrive() or between(), in a tile's first half, does).
+template <int D, int LOADS, typename Arrive, typename Request, typename Between>
 __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, const bf16x8 (&qf)[Tile<D>::KS], int lim,
-                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[Tile<D>::DB], float& m, float& l, Arrive arrive, Request request) {
+                                          int first_lim, unsigned kat, unsigned vat, f32x16 (&o)[Tile<D>::DB], float& m, float& l, Arrive arrive, Request request, Between between) {
     using X = Tile<D>;
     constexpr int ROW = D * 2, HALF = kWideTile * ROW, STAGE = 2 * HALF;
     constexpr int QS = X::KS, VS = 2 * X::DB;   // slots: products of 32 keys with K and with V
@@ -927,6 +927,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         const unsigned after = ((j + 1) >> 1) % kStages * STAGE + ((j + 1) & 1) * 32 * ROW;
         // the tile of the next step's K, so that its first pieces are read beside the products with V
         if ((j & 1) != 0 && j + 1 < 2 * hi) have = arrive(false, after) << 2;
+        if ((j & 1) == 0) between();
 #pragma unroll
         for (int i = 0; i < VS; ++i) {
             __builtin_amdgcn_sched_barrier(0);
@@ -967,6 +968,7 @@ __device__ __forceinline__ void wide_rows(const PagedParams& p, int lo, int hi, 
         multiply_k(sa, i, k);
     }
     mfma_done(sa);
+    between();
     mask(sa, lo * kWideTile, have);
 #pragma unroll
     for (int r = 0; r < PAIRS; ++r) look(sa, r);
@@ -1078,11 +1080,14 @@ __device__ __forceinline__ void wide_segment(const P& p, const Segment& g, unsig
     int arrives = g.lo;  // the tile that arrives next
     // The next tile is in LDS for everybody; everybody has left the tile before the last behind, whose stage the next requests take.  Loads behind
     // the tile's that are on their way: K and V of the next one at first, then K and half of V of the next one.
-    // An MXFP8 cache's next tile goes from registers to LDS here, and the one behind it is requested: nobody reads its stage any more, the slowest wavefront is at the
-    // tile before the last.
-    auto arrive_tile = [&](bool first, unsigned stage_at) {
+    // An MXFP8 cache's next tile goes from registers to LDS and the one behind it is requested: at D = 128 in the first half of the tile before it, when nobody reads its stage
+    // any more, so that a wavefront converts while the other of its SIMD multiplies; at D = 64, where the vector units have the more to do, in front of the barrier, where all do at
+    // once.  (2 chunks of 2048 behind 8192, 40 / 8 heads, D = 128: 791 us, all at once 802, a prompt of 2039 96 and 102; 32 / 8 heads, D = 64: the chunks 492 and 454, a
+    // chunk of 500 beside 31 branches 69 and 65.)
+    constexpr bool BETWEEN = kMx<P> && D == 128;
+    auto put_tile = [&](unsigned stage_at) {
+        const int have = have_0;
         if constexpr (kMx<P>) {
-            const int have = have_0;
             k8.put(to + stage_at, wave * KEYS, lane);
             v8.put(to + stage_at + HALF, wave * KEYS, lane);
             if (++arrives < g.hi) fetch8(arrives);
@@ -1093,6 +1098,17 @@ __device__ __forceinline__ void wide_segment(const P& p, const Segment& g, unsig
                 for (int i = 0; i < LOADS; ++i) taken_out |= keep_finite(to + stage_at + HALF + i * 1024 + lane * 16);
                 if (taken_out) sh_bad[wave] = 1;
             }
+        }
+        return have;
+    };
+    auto between = [&] {
+        if constexpr (BETWEEN) {
+            if (arrives < g.hi) have_1 = put_tile(arrives % kStages * STAGE);
+        }
+    };
+    auto arrive_tile = [&](bool first, unsigned stage_at) {
+        if constexpr (kMx<P>) {
+            const int have = first || !BETWEEN ? put_tile(stage_at) : have_1;
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             return have;
         }
@@ -1123,16 +1139,18 @@ __device__ __forceinline__ void wide_segment(const P& p, const Segment& g, unsig
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
     if (wave * 32 < g.nrows) {
-        wide_rows<D, kMx<P> ? 0 : LOADS>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request);
+        wide_rows<D, kMx<P> ? 0 : LOADS>(p, g.lo, g.hi, qf, lim, first_lim, kat, vat, oacc, m_run, l_run, arrive_tile, request, between);
     } else {  // no rows: the loads and the meetings alone, in the same order
         constexpr int N = kMx<P> ? 0 : LOADS;
         arrive_tile(true, g.lo % kStages * STAGE);
+        between();
 #pragma unroll
         for (int i = 0; i < N; ++i) request(g.lo + 2, 0, i);
         for (int j = g.lo; j + 1 < g.hi; ++j) {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) request(j + 2, 1, i);
             arrive_tile(false, (j + 1) % kStages * STAGE);
+            between();
 #pragma unroll
             for (int i = N / 2; i < N; ++i) request(j + 2, 1, i);
 #pragma unroll
