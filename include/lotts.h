@@ -439,7 +439,7 @@ int kv_pages_copy(void *pool, int32_t planes, int32_t pages, int64_t plane_strid
  * mxfp4_quantize -- a weight matrix to MXFP4, once, when it is loaded (Section 3.1: the step is bound by loading the weights; in this form
  * they are 4.25 bits each).  mxfp4_dequantize -- the values that such a matrix stands for, exact in both types.
  *   W, values [N][K] dtype (LOTTS_BF16 or LOTTS_F32; row pitch ldw, ld elements), codes [N][K / 2] bytes (ld_codes), scales [N][K / 32] bytes (ld_scales)
- *   K a multiple of 32; N * K < 2^34; W, values and codes 16-byte aligned, their pitches multiples of 16 bytes
+ *   K a multiple of 32; N * K < 2^34; W, values and codes 16-byte aligned, their pitches multiples of 16 bytes (of one row any that are not too short)
  */
 int mxfp4_quantize(int32_t N, int32_t K, lotts_dtype dtype, const void *W, int64_t ldw, void *codes, int64_t ld_codes, void *scales,
                    int64_t ld_scales, void *stream);
@@ -453,7 +453,7 @@ size_t skinny_gemm_mxfp4_workspace_bytes(int32_t M, int32_t N, int32_t K);
  * skinny_gemm_mxfp4 -- skinny_gemm against a weight matrix in MXFP4: Y[m][n] = sum_k X[m][k] * W[n][k], W what codes and scales stand for.
  *   X [M][K] bf16 (row pitch ldx elements), codes [N][K / 2] (ld_codes bytes), scales [N][K / 32] (ld_scales bytes), Y [M][N] bf16 out (ldy elements)
  *   1 <= M <= 256; any N; K a multiple of 32 (both up to 2^22); X, codes, workspace 16-byte aligned, ldx a multiple of 8 up to 2^22, ld_codes of 16; Y and scales
- *   as they are; ld_codes, ld_scales up to 2^24
+ *   as they are; ld_codes, ld_scales up to 2^24 (of one row, of X or of W, any pitch that is not too short)
  * The weights become bf16, exactly, and the products accumulate in fp32 on the matrix cores, in an order that the sizes decide: the same data give the same bits.
  *   workspace: >= skinny_gemm_mxfp4_workspace_bytes(M, N, K), any contents
  */

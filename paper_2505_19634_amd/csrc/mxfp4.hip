@@ -52,7 +52,9 @@ static int mx4_params(Mx4Params* p, int32_t N, int32_t K, int dtype, const void*
     const long long es = dtype == LOTTS_BF16 ? 2 : 4;
     if (N < 1 || K < kMxBlock || K % kMxBlock != 0 || (long long)N * (K / 8) > 0x7fffffffLL - 256) return LOTTS_ERR_SHAPE;
     if (!values || !codes || !scales) return LOTTS_ERR_NULL;
-    if (ld < K || ld_codes < K / 2 || ld_scales < K / kMxBlock || ld % (16 / es) != 0 || ld_codes % 16 != 0) return LOTTS_ERR_SHAPE;
+    if (ld < K || ld_codes < K / 2 || ld_scales < K / kMxBlock) return LOTTS_ERR_SHAPE;
+    if (N == 1) ld = K, ld_codes = K / 2, ld_scales = K / kMxBlock;  // of one row the pitches are nobody's
+    if (ld % (16 / es) != 0 || ld_codes % 16 != 0) return LOTTS_ERR_SHAPE;
     if (ld > (1LL << 56) || ld_codes > (1LL << 58) / N || ld_scales > (1LL << 58) / N || ld > (1LL << 58) / N) return LOTTS_ERR_SHAPE;  // 64-bit offsets
     if ((((uintptr_t)values | (uintptr_t)codes) & 15) != 0) return LOTTS_ERR_SHAPE;
     p->codes = static_cast<unsigned char*>(const_cast<void*>(codes));

@@ -447,7 +447,10 @@ extern "C" int skinny_gemm_mxfp4(int32_t M, int32_t N, int32_t K, const void* X,
     using namespace lotts;
     if (!gemm4_sizes(M, N, K)) return LOTTS_ERR_SHAPE;
     if (!X || !codes || !scales || !Y || !workspace) return LOTTS_ERR_NULL;
-    if (ldx < K || ld_codes < K / 2 || ld_scales < K / kMxBlock || ldy < N || ldx % 8 != 0 || ld_codes % 16 != 0) return LOTTS_ERR_SHAPE;
+    if (ldx < K || ld_codes < K / 2 || ld_scales < K / kMxBlock || ldy < N) return LOTTS_ERR_SHAPE;
+    if (M == 1) ldx = K;  // of one row the pitch is nobody's: the last token of a context, a row of a matrix of any pitch
+    if (N == 1) ld_codes = K / 2, ld_scales = K / kMxBlock;
+    if (ldx % 8 != 0 || ld_codes % 16 != 0) return LOTTS_ERR_SHAPE;
     // a workgroup's rows of codes and scales, and all tokens, lie within 2^31 bytes of the first; 64-bit offsets hold all of Y
     if (ldx > (1 << 22) || ld_codes > (1 << 24) || ld_scales > (1 << 24) || ldy > (1LL << 48)) return LOTTS_ERR_SHAPE;
     if ((((uintptr_t)X | (uintptr_t)codes | (uintptr_t)workspace) & 15) != 0 || ((uintptr_t)Y & 1) != 0) return LOTTS_ERR_SHAPE;
