@@ -432,7 +432,8 @@ int kv_pages_copy(void *pool, int32_t planes, int32_t pages, int64_t plane_strid
  * The calls that quantise choose the smallest power of two with which no value of the block lies behind the largest element, within s = 2 .. 252 (MXFP4) and
  * 10 .. 246 (MXFP8), where everything that a block stands for is a normal bf16 or zero; every element is the nearest to its value, ties to the even one, and
  * keeps its sign.  (Values beyond 1.5 * 2^127, MXFP4, and 1.75 * 2^127, MXFP8, become these.)  A block with an infinity or a NaN gets s = 255 and is NaN throughout.
- * The calls that read take any bytes: s = 255 makes a block NaN; where an element times its power of two is no bf16 it is rounded to one.
+ * The calls that read take any bytes: s = 255 makes a block NaN; where an element times its power of two is no bf16 it is rounded to one, the nearest, ties to
+ * the even one, infinite from 2^128 on (fp32 rows of verify_attention_paged_mxfp8 read it as it is, fp32 holds it).
  */
 
 /*

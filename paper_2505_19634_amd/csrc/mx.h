@@ -73,7 +73,8 @@ __device__ __forceinline__ unsigned mx_to_e2m1(const float (&x)[8], unsigned s) 
     return s == kMxNaN ? 0 : w;
 }
 
-// Eight elements as bf16, exact; scale 255 makes every element NaN.
+// Eight elements as bf16, exact under the scales that are written here; under others (below 2^-126 bf16 has fewer bits) the nearest, ties to the even one, infinite
+// from 2^128 on.  Scale 255 makes every element NaN.
 __device__ __forceinline__ mx_bf16x8 mx_of_e2m1(unsigned w, unsigned s) {
     const float scale = mx_power(s);
     const mx_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1),
@@ -86,7 +87,7 @@ __device__ __forceinline__ mx_bf16x8 mx_of_e4m3(unsigned lo, unsigned hi, unsign
                     c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return mx_bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// Four e4m3 elements as fp32, exact.
+// Four e4m3 elements as fp32, exact under any scale, infinite from 2^128 on.
 __device__ __forceinline__ float4 mx_f32_of_e4m3(unsigned w, unsigned s) {
     const mx_f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, mx_power(s), false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, mx_power(s), true);
     return make_float4(a[0], a[1], b[0], b[1]);
