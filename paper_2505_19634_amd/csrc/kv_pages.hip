@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256) void kv_append_paged_kernel(const AppendPagedP
 
 // ---------------------------------------------------------------------------------------------
 // kv_append_paged_mxfp8: the same, and the rows become 8-bit microscaled numbers (mx.h) on the way.  A lane has eight values of K and
-// of V at a time, four lanes a block.  6274 tokens of 8 heads of 128, 39 MB, 9.0 us (4.3 TB/s); 64 tokens 4.1, the launch.
+// of V at a time, four lanes a block.  6274 tokens of 8 heads of 128, 39 MB, 9.1 us (4.3 TB/s); 64 tokens 4.1, the launch.
 // ---------------------------------------------------------------------------------------------
 struct AppendPagedMxParams : AppendPagedParams {  // pieces: of eight values
     unsigned char *Kscales, *Vscales;

@@ -1,8 +1,8 @@
 // mxfp4_quantize, mxfp4_dequantize: a weight matrix to 4-bit microscaled numbers (mx.h), once, when it is loaded, and back to the values that these
 // stand for.  The verify forward streams its weights once a step (paper Section 3.1: the step is bound by loading them); in this form they are
 // 4.25 bits each.  A lane has eight neighbouring values, four lanes a block; every load and store of a wavefront is one piece of memory.
-// Bound by HBM: 55296 x 5120 bf16, 716 MB, 121 us (5.9 TB/s), 119 back; fp32 222.  (Two, four and eight pieces a lane requested at once 121, 126, 131; stores that
-// pass the caches by 131, fp32 212.)
+// Bound by HBM: 55296 x 5120 bf16, 716 MB, one call behind another 121 us (5.9 TB/s), 130 back; in turn, among each other's writes, 141 and 119; fp32 222.
+// (Two, four and eight pieces a lane requested at once 121, 126, 131; stores that pass the caches by 131, fp32 212.)
 #include "mx.h"
 
 namespace lotts {
